@@ -60,6 +60,12 @@ extern "C" {
 #define KRONQ_BF16 1
 #define KRONQ_FP32 2
 
+/* ---- activations of the served layer ------------------------------------------------------ */
+#define KRONQ_ACT_NONE 0
+#define KRONQ_ACT_RELU 1 /* max(z, 0) */
+#define KRONQ_ACT_GELU 2 /* z (1 + erf(z / sqrt 2)) / 2 */
+#define KRONQ_ACT_SILU 3 /* z / (1 + exp(-z)) */
+
 /* ---- kronq_rotate flags ------------------------------------------------------------------ */
 #define KRONQ_RESCALE_IN 1   /* S_X = diag(H_X,jj / ||W_:,j||^2)^(1/4)        (eq. rescale) */
 #define KRONQ_RESCALE_OUT 2  /* S_G = diag(H_G,ii / ||W_i,:||^2)^(1/4)        (eq. rescale) */
@@ -104,6 +110,8 @@ extern "C" {
 #define KRONQ_OP_EIGH 12         /* kronq_eigh: d as d_in */
 #define KRONQ_OP_PROXY 13        /* kronq_proxy_loss_factors: d_out, d_in */
 #define KRONQ_OP_COV_DIAG 14     /* kronq_cov_diag: d as d_in, tokens as n_rows */
+#define KRONQ_OP_LINEAR 15       /* kronq_online_linear: d_out, d_in, n_rows */
+#define KRONQ_OP_ATTENTION 16    /* kronq_cache_attention: n_heads as d_out, dim as d_in, n_tokens as n_rows */
 
 /* Bytes of scratch the operation needs for these sizes. For KRONQ_OP_COV pass the covariance
  * dimension d as d_in and the token count as n_rows (d_out ignored); for KRONQ_OP_CHOL pass
@@ -340,6 +348,112 @@ int kronq_online_matvec(const uint32_t* packed, int64_t ldp, const float* scales
                         const float* q28_in, const float* q28_out, int flags, const void* x,
                         int x_dtype, int64_t ldx, int64_t batch, float* y, int64_t ldy, void* ws,
                         size_t ws_bytes, void* stream);
+
+/* ---- 7a. the served layer on any number of rows --------------------------------------------
+ * y[t] = act(diag(mul_out) T_out W_hat' T_in diag(mul_in) x[t] + bias) + residual[t] for
+ * t < n_rows: kronq_online_matvec's product (same packed codes, scales, factors, flags) for one
+ * token, a decode batch or whole prompts.
+ *   zeros    here integers in [-1024, 1023] (the sweep's lie in [0, 2^bits)).
+ *   x        device [n_rows x ldx], KRONQ_BF16 or KRONQ_FP32, 16-byte aligned rows.
+ *   bias     device fp32 [d_out], 4-byte aligned, or NULL.
+ *   act      KRONQ_ACT_*.
+ *   residual device [n_rows x ldr], y's type, or NULL; may be y itself.
+ *   y        device [n_rows x ldy], y_dtype KRONQ_BF16 or KRONQ_FP32, rows aligned to the element;
+ *            must not overlap x.
+ * Precision: a KRONQ_BF16 result takes the transformed activations and, with many rows, the
+ * dequantised weights rounded to fp16 (each row scaled by a power of two; a quantisation group
+ * whose scale is below 2^-8 of its row's largest keeps fewer than 11 bits), summed in fp32. A
+ * KRONQ_FP32 result takes activations of 22 bits (none coarser than 2^-32 of the row's largest)
+ * and exact weights. Up to 4 rows with n_rows * d_in <= 32768 take kronq_online_matvec's.
+ * n_rows = 0 does nothing. d_in <= 32768 (a multiple of 128), d_out <= 32768, n_rows <= 2^24.
+ * Workspace: KRONQ_OP_LINEAR. */
+int kronq_online_linear(const uint32_t* packed, int64_t ldp, const float* scales,
+                        const float* zeros, int64_t ldsz, int bits, int group, int64_t d_out,
+                        int64_t d_in, const float* mul_in, const float* mul_out,
+                        const float* q28_in, const float* q28_out, int flags, const void* x,
+                        int x_dtype, int64_t ldx, int64_t n_rows, const float* bias, int act,
+                        const void* residual, int64_t ldr, void* y, int y_dtype, int64_t ldy,
+                        void* ws, size_t ws_bytes, void* stream);
+
+/* ---- 7b. the served layers of a mixture of experts ------------------------------------------
+ * kronq_online_linear with one layer per expert, for rows sorted by expert: rows offsets[e] to
+ * offsets[e + 1] - 1 of x, residual and y belong to expert e. The experts share bits, group,
+ * sizes, flags and act; their layers follow one another: packed [n_experts * d_out x ldp], scales
+ * and zeros [n_experts * d_out x ldsz], mul_in [n_experts x d_in], mul_out and bias
+ * [n_experts x d_out], q28_in and q28_out [n_experts x 28 x 28].
+ *   offsets  device int32 [n_experts + 1], ascending (equal: no rows). Read on the device, so a
+ *            captured call follows what a router writes there. Values outside [0, n_rows] are cut
+ *            to it, one below its predecessor is raised to it (the results of such experts are
+ *            undefined; nothing outside the rows is touched).
+ *   Rows before offsets[0] and from offsets[n_experts] on keep what y holds.
+ *   1 <= n_experts <= 4096, n_experts * d_out <= 2^31 - 1.
+ * Workspace: kronq_grouped_workspace_bytes. */
+int kronq_online_grouped(const uint32_t* packed, int64_t ldp, const float* scales,
+                         const float* zeros, int64_t ldsz, int bits, int group, int64_t d_out,
+                         int64_t d_in, const float* mul_in, const float* mul_out,
+                         const float* q28_in, const float* q28_out, int flags, const void* x,
+                         int x_dtype, int64_t ldx, int64_t n_rows, const int32_t* offsets,
+                         int64_t n_experts, const float* bias, int act, const void* residual,
+                         int64_t ldr, void* y, int y_dtype, int64_t ldy, void* ws,
+                         size_t ws_bytes, void* stream);
+/* Bytes of scratch of kronq_online_grouped for these sizes (0 for invalid ones). Host only. */
+size_t kronq_grouped_workspace_bytes(int64_t d_out, int64_t d_in, int64_t n_rows,
+                                     int64_t n_experts);
+
+/* ---- 7c. keys and values in a cache of 4-bit codes --------------------------------------------
+ * The cache holds, for every slot (token place) and kv head, a key and a value of dim values on
+ * the min-max grid of 16 levels: r = v, or r = H v / sqrt(dim) with rotate (the Sylvester
+ * Hadamard, which spreads strong channels over the row; kronq_cache_attention then turns queries
+ * and outputs alike), and
+ *   scale = (max(0, max r) - min(0, min r)) / 15, at least 2^-100, rounded up to bf16,
+ *   zero = rint(-min(0, min r) / scale), code = clamp(rint(r / scale) + zero, 0, 15),
+ * in fp64, rint half to even. A row with a value that is not finite (or beyond 3e38) reads as NaN.
+ *   codes   device uint32 [n_pages][n_kv][2][page * dim / 8], 16-byte aligned: keys (0) as
+ *           [token][dim / 8], values (1) as [token / 4][dim / 8][token % 4]; a word holds eight
+ *           consecutive codes, low bits first.
+ *   params  device uint32 [n_pages][n_kv][2][page], 16-byte aligned: the scale's bf16 bits in the
+ *           upper half, the zero in the lower.
+ * kronq_cache_append writes the tokens' rows at slots[t] = page index * page + place (int64,
+ * device). A negative slot, or one from n_pages * page on, leaves its token out. Slots of one call
+ * are distinct.
+ *   k, v    device [n_tokens][n_kv][dim], dtype KRONQ_BF16 or KRONQ_FP32, tokens ldk / ldv
+ *           elements apart; 16-byte aligned, ldk and ldv divisible by 8 (bf16) or 4 (fp32).
+ *   k_hat, v_hat  device fp32 [n_tokens][n_kv][dim], 16-byte aligned, or NULL: the values that the
+ *           codes stand for, scale * (code - zero) (of r), for the tokens that were written.
+ *   dim is 64 or 128; page a power of two from 16 to 65536. n_tokens = 0 does nothing. */
+int kronq_cache_append(const void* k, const void* v, int dtype, int64_t ldk, int64_t ldv,
+                       int64_t n_tokens, int64_t n_kv, int64_t dim, const int64_t* slots,
+                       uint32_t* codes, uint32_t* params, int64_t n_pages, int64_t page,
+                       int rotate, float* k_hat, float* v_hat, void* stream);
+
+/* Attention of new tokens over the cache, for decoding (one new token per sequence) and for
+ * prompts packed one after another:
+ *   out[t][h] = sum_s p_s V_s,  p = softmax over the visible s of scale * q[t][h] . K_s
+ * with K and V of kv head h / (n_heads / n_kv). Tokens starts[b] to starts[b + 1] - 1 of q are the
+ * last ones of sequence b, whose lengths[b] cached tokens include them: its i-th of n new tokens
+ * sees cached tokens 0 to lengths[b] - n + i. A token that sees none gets zeros.
+ *   q, out   device bf16 [n_tokens][n_heads][dim], tokens ldq / ldo elements apart; q 16-byte
+ *            aligned with ldq divisible by 8, out 2-byte aligned.
+ *   table    device int32 [n_seqs x ldt]: the page of tokens j * page to j * page + page - 1 of
+ *            sequence b in column j, table_pages columns. Tokens on a page outside [0, n_pages)
+ *            are not seen.
+ *   lengths  device int32 [n_seqs]; cut to [0, table_pages * page].
+ *   starts   device int32 [n_seqs + 1], ascending, cut to [0, n_tokens]; NULL: token b is the one
+ *            new token of sequence b (n_tokens <= n_seqs). Tokens of no sequence keep what out
+ *            holds.
+ *   max_new  host: at least one and about the largest number of new tokens of a sequence (it sizes
+ *            the launch; a longer one is computed all the same, later).
+ *   All of table, lengths and starts are read on the device, so that a captured call follows them.
+ * Precision: rotated queries and the weights p (times the value's scale) in fp16, the latter not
+ * coarser than 2^-25 of the largest value scale; sums in fp32.
+ *   n_heads a multiple of n_kv; dim, page, rotate as in kronq_cache_append; n_seqs <= 65535,
+ *   n_kv <= 65535. n_tokens = 0 does nothing. Workspace: KRONQ_OP_ATTENTION. */
+int kronq_cache_attention(const void* q, int64_t ldq, int64_t n_tokens, int64_t n_heads,
+                          int64_t n_kv, int64_t dim, const uint32_t* codes, const uint32_t* params,
+                          int64_t n_pages, int64_t page, const int32_t* table, int64_t ldt,
+                          int64_t table_pages, const int32_t* lengths, int64_t n_seqs,
+                          const int32_t* starts, int64_t max_new, float scale, int rotate,
+                          void* out, int64_t ldo, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- 8. diagnostics of the incoherence processing ------------------------------------------
  * (Sec. 2.3 eq. incoherence_measure; Sec. 4.2 and Fig. 2; Prop. 2 eq. biip-bound, appendix A.3

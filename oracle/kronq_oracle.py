@@ -76,6 +76,7 @@ __all__ = [
     "allocate_bits", "count_avg_bits", "dequantize", "online_matvec", "pack_codes",
     "incoherence", "norm_cv", "eigenvectors", "hessian_incoherence", "sweep_pivots",
     "rescale_objective", "rescale_gain", "proxy_loss_factors",
+    "served_linear", "round_up_bf16", "cache_grid", "cache_words", "causal_attention",
     "RESCALE_IN", "RESCALE_OUT", "ROT_IN", "ROT_OUT", "BIIP",
 ]
 
@@ -594,3 +595,70 @@ def proxy_loss_factors(HG, W, Hd, U=None) -> dict:
             "gptq": float(np.sum(h) * np.sum(a) * trD),
             "kronq": float(np.sum(np.sqrt(h * a)) ** 2 * trD),
             "rho": rescale_gain(h, a), "trD": trD, "trH": trH}
+
+
+# ------------------------------------------------------------------- serving (rows, cache, attention)
+def served_linear(w_rot, mul_in, mul_out, V, U, x, bias=None, act="none", residual=None):
+    """act(diag(mul_out) T_out W' T_in diag(mul_in) x + bias) + residual for the rows of x: V and U
+    are the dense factors T_in and T_out (signs and rescaling are in the multipliers)."""
+    z = ((((x * mul_in) @ V.T) @ w_rot.T) @ U.T) * mul_out
+    if bias is not None:
+        z = z + bias
+    if act == "relu":
+        z = np.maximum(z, 0.0)
+    elif act == "silu":
+        z = z / (1.0 + np.exp(-z))
+    elif act == "gelu":
+        from scipy.special import erf
+        z = 0.5 * z * (1.0 + erf(z / np.sqrt(2.0)))
+    return z if residual is None else z + residual
+
+
+def round_up_bf16(v):
+    """The smallest bf16 value not below each (positive, normal) v."""
+    _, e = np.frexp(v)
+    unit = np.ldexp(1.0, e - 8)
+    return np.ceil(v / unit) * unit
+
+
+def cache_grid(v, rotate):
+    """Codes, scale and zero of the rows of v on the cache's 16-level grid, and the values held."""
+    r = np.asarray(v, dtype=np.float64)
+    if rotate:
+        r = r @ hadamard(r.shape[-1]) / np.sqrt(r.shape[-1])
+    lo, hi = np.minimum(r.min(-1), 0.0), np.maximum(r.max(-1), 0.0)
+    scale = round_up_bf16(np.maximum((hi - lo) / 15.0, 2.0 ** -100))
+    zero = np.minimum(np.rint(-lo / scale), 15.0)
+    codes = np.clip(np.rint(r / scale[..., None]) + zero[..., None], 0, 15)
+    return codes.astype(np.int64), scale, zero.astype(np.int64), scale[..., None] * (
+        codes - zero[..., None])
+
+
+def cache_words(codes, part):
+    """Packed words of a page of codes [page, dim]: keys (0) token by token, values (1) with four
+    tokens interleaved."""
+    page, dim = codes.shape
+    words = np.zeros((page, dim // 8), dtype=np.uint32)
+    for j in range(8):
+        words |= codes[:, j::8].astype(np.uint32) << np.uint32(4 * j)
+    if part:
+        words = words.reshape(page // 4, 4, dim // 8).transpose(0, 2, 1)
+    return words.reshape(-1)
+
+
+def causal_attention(q, k, v, scale):
+    """New tokens q [new, heads, dim] as the last of the tokens k, v [tokens, kv heads, dim]; a query
+    that sees no token gives zeros."""
+    new, heads, _ = q.shape
+    tokens, kv = k.shape[:2]
+    out = np.zeros_like(q, dtype=np.float64)
+    for i in range(new):
+        seen = tokens - new + i + 1
+        if seen <= 0:
+            continue
+        for h in range(heads):
+            g = h // (heads // kv)
+            s = scale * (k[:seen, g] @ q[i, h])
+            p = np.exp(s - s.max())
+            out[i, h] = (p / p.sum()) @ v[:seen, g]
+    return out

@@ -161,6 +161,66 @@ int online_matvec_launch(const uint32_t* packed, int64_t ldp, const float* scale
                          const float* q28_in, const float* q28_out, int flags, const void* x,
                          int x_dtype, int64_t ldx, int64_t batch, float* y, int64_t ldy, void* ws,
                          hipStream_t s);
+int online_product_launch(const uint32_t* packed, int64_t ldp, const float* scales,
+                          const float* zeros, int64_t ldsz, int bits, int group, int64_t d_out,
+                          int64_t d_in, const float* mul_in, const float* q28_in, int flags,
+                          const void* x, int x_dtype, int64_t ldx, int64_t batch, void* ws,
+                          float** y_rot, hipStream_t s);
+// the served layer on any number of rows (offsets null: one layer)
+struct LinearJob {
+  const uint32_t* packed;
+  int64_t ldp;
+  const float *scales, *zeros;
+  int64_t ldsz;
+  int bits, group;
+  int64_t d_out, d_in;
+  const float *mul_in, *mul_out, *q28_in, *q28_out;
+  int flags;
+  const void* x;
+  int x_dtype;
+  int64_t ldx, n_rows;
+  const int* offsets;
+  int64_t n_experts;
+  const float* bias;
+  int act;
+  const void* residual;
+  int64_t ldr;
+  void* y;
+  int y_dtype;
+  int64_t ldy;
+};
+size_t linear_ws_bytes(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts);
+int linear_launch(const LinearJob& j, void* ws, hipStream_t s);
+// the 4-bit key/value cache
+struct AppendJob {
+  const void *k, *v;
+  int dtype;
+  int64_t ldk, ldv, n_tokens, n_kv, dim;
+  const int64_t* slots;
+  uint32_t *codes, *params;
+  int64_t n_pages, page;
+  int rotate;
+  float *k_hat, *v_hat;
+};
+int cache_append_launch(const AppendJob& j, hipStream_t s);
+struct AttentionJob {
+  const void* q;
+  int64_t ldq, n_tokens, n_heads, n_kv, dim;
+  const uint32_t *codes, *params;
+  int64_t n_pages, page;
+  const int32_t* table;
+  int64_t ldt, table_pages;
+  const int32_t* lengths;
+  int64_t n_seqs;
+  const int32_t* starts;
+  int64_t max_new;
+  float scale;
+  int rotate;
+  void* out;
+  int64_t ldo;
+};
+size_t attention_ws_bytes(int64_t n_heads, int64_t dim, int64_t n_tokens);
+int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s);
 // diagnostics: matrix statistics, Jacobi eigendecomposition, expected-loss factors
 size_t matrix_stats_ws_bytes(int64_t rows, int64_t cols);
 int matrix_stats_launch(const void* M, int dtype, int64_t rows, int64_t cols, int64_t ld,

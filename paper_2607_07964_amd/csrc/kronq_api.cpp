@@ -90,6 +90,70 @@ int obs_common(float* W, int64_t d_out, int64_t d_in, int64_t ldw, const float* 
                         err, W_hat, ws, as_stream(stream));
 }
 
+// the served layer for rows (one layer: offsets NULL and one expert)
+int linear_common(const kq::LinearJob& j, void* ws, size_t ws_bytes, void* stream) {
+  KQ_REQUIRE((j.flags & ~KRONQ_BIIP) == 0, KRONQ_ERR_INVALID_ARG, "unknown flag bits 0x%x",
+             j.flags & ~KRONQ_BIIP);
+  KQ_REQUIRE(j.bits == 2 || j.bits == 3 || j.bits == 4 || j.bits == 8, KRONQ_ERR_UNSUPPORTED,
+             "bits must be 2, 3, 4 or 8");
+  KQ_REQUIRE(j.act >= KRONQ_ACT_NONE && j.act <= KRONQ_ACT_SILU, KRONQ_ERR_INVALID_ARG,
+             "unknown activation %d", j.act);
+  KQ_REQUIRE(j.d_out >= 1 && j.d_in >= 128 && j.n_rows >= 0 && j.n_rows <= (int64_t(1) << 24),
+             KRONQ_ERR_INVALID_ARG, "bad sizes");
+  KQ_REQUIRE(j.group >= 128 && j.group % 128 == 0 && j.d_in % j.group == 0, KRONQ_ERR_SHAPE,
+             "group must be a multiple of 128 dividing d_in");
+  KQ_REQUIRE(j.d_in <= kMaxRotDim && j.d_out <= kMaxRotDim, KRONQ_ERR_UNSUPPORTED,
+             "d_in and d_out must be at most %lld: a row must fit the LDS", (long long)kMaxRotDim);
+  KQ_REQUIRE(j.n_experts * j.d_out <= 0x7FFFFFFF, KRONQ_ERR_UNSUPPORTED,
+             "n_experts * d_out must be below 2^31");
+  KQ_REQUIRE(j.packed && aligned(j.packed, 16) && j.ldp % 4 == 0 &&
+                 j.ldp >= j.d_in * j.bits / 32,
+             KRONQ_ERR_INVALID_ARG,
+             "packed must be 16-byte aligned with ldp >= d_in * bits / 32, divisible by 4");
+  KQ_REQUIRE(j.scales && j.zeros && aligned(j.scales, 4) && aligned(j.zeros, 4) &&
+                 j.ldsz >= j.d_in / j.group,
+             KRONQ_ERR_INVALID_ARG, "bad scales or zeros");
+  KQ_REQUIRE(aligned(j.mul_in, 16) && aligned(j.mul_out, 16) && aligned(j.bias, 4),
+             KRONQ_ERR_INVALID_ARG, "mul_in and mul_out must be 16-byte aligned, bias 4");
+  KQ_REQUIRE(valid_dtype(j.x_dtype) && valid_dtype(j.y_dtype), KRONQ_ERR_INVALID_ARG,
+             "x and y must be KRONQ_BF16 or KRONQ_FP32");
+  for (int side = 0; side < 2; ++side) {
+    if (!(j.flags & (side ? KRONQ_ROT_OUT : KRONQ_ROT_IN))) continue;
+    const int64_t d = side ? j.d_out : j.d_in;
+    const float* q28 = side ? j.q28_out : j.q28_in;
+    const kq::RotDim r = kq::rot_dim(d);
+    KQ_REQUIRE(r.ok, KRONQ_ERR_UNSUPPORTED, "%s dimension %lld is not 2^k or 28*2^k",
+               side ? "output" : "input", (long long)d);
+    KQ_REQUIRE(!r.has28 || (q28 && aligned(q28, 4)), KRONQ_ERR_INVALID_ARG,
+               "%s dimension 28 * 2^k needs the 28 x 28 factor", side ? "output" : "input");
+  }
+  if (j.n_rows == 0) return KRONQ_OK;
+  KQ_REQUIRE(j.x && aligned(j.x, 16) && j.ldx >= j.d_in &&
+                 j.ldx % (j.x_dtype == KRONQ_BF16 ? 8 : 4) == 0,
+             KRONQ_ERR_INVALID_ARG,
+             "x must be 16-byte aligned with ldx >= d_in divisible by 8 (bf16) or 4 (fp32)");
+  const size_t ye = j.y_dtype == KRONQ_BF16 ? 2 : 4;
+  KQ_REQUIRE(j.y && aligned(j.y, ye) && j.ldy >= j.d_out, KRONQ_ERR_INVALID_ARG,
+             "y is NULL or misaligned, or ldy < d_out");
+  KQ_REQUIRE(!j.residual || (aligned(j.residual, ye) && j.ldr >= j.d_out), KRONQ_ERR_INVALID_ARG,
+             "residual is misaligned, or ldr < d_out");
+  KQ_TRY(check_ws(ws, ws_bytes, kq::linear_ws_bytes(j.d_out, j.d_in, j.n_rows, j.n_experts)));
+  return kq::linear_launch(j, ws, as_stream(stream));
+}
+
+// the paged cache of 4-bit keys and values
+int check_cache(const uint32_t* codes, const uint32_t* params, int64_t n_pages, int64_t page,
+                int64_t n_kv, int64_t dim) {
+  KQ_REQUIRE(dim == 64 || dim == 128, KRONQ_ERR_UNSUPPORTED, "dim must be 64 or 128");
+  KQ_REQUIRE(page >= 16 && page <= 65536 && (page & (page - 1)) == 0, KRONQ_ERR_UNSUPPORTED,
+             "page must be a power of two from 16 to 65536");
+  KQ_REQUIRE(n_kv >= 1 && n_kv <= 65535 && n_pages >= 1 && n_pages <= 0x7FFFFFFF,
+             KRONQ_ERR_INVALID_ARG, "bad n_kv or n_pages");
+  KQ_REQUIRE(codes && params && aligned(codes, 16) && aligned(params, 16), KRONQ_ERR_INVALID_ARG,
+             "codes and params must be 16-byte aligned device pointers");
+  return KRONQ_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -110,6 +174,10 @@ size_t kronq_workspace_bytes(int op, int64_t d_out, int64_t d_in, int64_t n_rows
       return kq::obs_ws_bytes(d_out, d_in, true);
     case KRONQ_OP_ONLINE:
       return kq::online_ws_bytes(d_out, d_in, n_rows);
+    case KRONQ_OP_LINEAR:
+      return kq::linear_ws_bytes(d_out, d_in, n_rows, 1);
+    case KRONQ_OP_ATTENTION:
+      return kq::attention_ws_bytes(d_out, d_in, n_rows);
     case KRONQ_OP_STATS:
       return kq::matrix_stats_ws_bytes(d_out, d_in);
     case KRONQ_OP_EIGH:
@@ -484,6 +552,107 @@ int kronq_online_matvec(const uint32_t* packed, int64_t ldp, const float* scales
   return kq::online_matvec_launch(packed, ldp, scales, zeros, ldsz, bits, group, d_out, d_in,
                                   mul_in, mul_out, q28_in, q28_out, flags, x, x_dtype, ldx, batch,
                                   y, ldy, ws, as_stream(stream));
+}
+
+int kronq_online_linear(const uint32_t* packed, int64_t ldp, const float* scales,
+                        const float* zeros, int64_t ldsz, int bits, int group, int64_t d_out,
+                        int64_t d_in, const float* mul_in, const float* mul_out,
+                        const float* q28_in, const float* q28_out, int flags, const void* x,
+                        int x_dtype, int64_t ldx, int64_t n_rows, const float* bias, int act,
+                        const void* residual, int64_t ldr, void* y, int y_dtype, int64_t ldy,
+                        void* ws, size_t ws_bytes, void* stream) {
+  kq::clear_error();
+  const kq::LinearJob j{packed, ldp,     scales, zeros,  ldsz,     bits, group,   d_out,
+                        d_in,   mul_in,  mul_out, q28_in, q28_out, flags, x,       x_dtype,
+                        ldx,    n_rows,  nullptr, 1,      bias,    act,  residual, ldr,
+                        y,      y_dtype, ldy};
+  return linear_common(j, ws, ws_bytes, stream);
+}
+
+int kronq_online_grouped(const uint32_t* packed, int64_t ldp, const float* scales,
+                         const float* zeros, int64_t ldsz, int bits, int group, int64_t d_out,
+                         int64_t d_in, const float* mul_in, const float* mul_out,
+                         const float* q28_in, const float* q28_out, int flags, const void* x,
+                         int x_dtype, int64_t ldx, int64_t n_rows, const int32_t* offsets,
+                         int64_t n_experts, const float* bias, int act, const void* residual,
+                         int64_t ldr, void* y, int y_dtype, int64_t ldy, void* ws,
+                         size_t ws_bytes, void* stream) {
+  kq::clear_error();
+  KQ_REQUIRE(offsets && aligned(offsets, 4), KRONQ_ERR_INVALID_ARG,
+             "offsets is NULL or misaligned");
+  KQ_REQUIRE(n_experts >= 1 && n_experts <= 4096, KRONQ_ERR_UNSUPPORTED,
+             "1 <= n_experts <= 4096");
+  const kq::LinearJob j{packed, ldp,     scales,  zeros,     ldsz,    bits, group,    d_out,
+                        d_in,   mul_in,  mul_out, q28_in,    q28_out, flags, x,        x_dtype,
+                        ldx,    n_rows,  offsets, n_experts, bias,    act,  residual, ldr,
+                        y,      y_dtype, ldy};
+  return linear_common(j, ws, ws_bytes, stream);
+}
+
+size_t kronq_grouped_workspace_bytes(int64_t d_out, int64_t d_in, int64_t n_rows,
+                                     int64_t n_experts) {
+  return kq::linear_ws_bytes(d_out, d_in, n_rows, n_experts);
+}
+
+int kronq_cache_append(const void* k, const void* v, int dtype, int64_t ldk, int64_t ldv,
+                       int64_t n_tokens, int64_t n_kv, int64_t dim, const int64_t* slots,
+                       uint32_t* codes, uint32_t* params, int64_t n_pages, int64_t page,
+                       int rotate, float* k_hat, float* v_hat, void* stream) {
+  kq::clear_error();
+  KQ_REQUIRE(valid_dtype(dtype), KRONQ_ERR_INVALID_ARG, "dtype must be KRONQ_BF16 or KRONQ_FP32");
+  KQ_REQUIRE(n_tokens >= 0, KRONQ_ERR_INVALID_ARG, "n_tokens < 0");
+  KQ_TRY(check_cache(codes, params, n_pages, page, n_kv, dim));
+  const int64_t per16 = dtype == KRONQ_BF16 ? 8 : 4;
+  if (n_tokens == 0) return KRONQ_OK;
+  KQ_REQUIRE(k && v && aligned(k, 16) && aligned(v, 16) && ldk % per16 == 0 && ldv % per16 == 0,
+             KRONQ_ERR_INVALID_ARG,
+             "k and v must be 16-byte aligned with ldk, ldv divisible by 8 (bf16) or 4 (fp32)");
+  KQ_REQUIRE(n_tokens == 1 || (ldk >= n_kv * dim && ldv >= n_kv * dim), KRONQ_ERR_INVALID_ARG,
+             "ldk and ldv must be at least n_kv * dim");
+  KQ_REQUIRE(slots && aligned(slots, 8), KRONQ_ERR_INVALID_ARG, "slots is NULL or misaligned");
+  KQ_REQUIRE((!k_hat || aligned(k_hat, 16)) && (!v_hat || aligned(v_hat, 16)),
+             KRONQ_ERR_INVALID_ARG, "k_hat and v_hat must be 16-byte aligned");
+  KQ_REQUIRE(n_tokens <= (int64_t(1) << 31) / n_kv, KRONQ_ERR_UNSUPPORTED,
+             "n_tokens * n_kv must be at most 2^31");
+  const kq::AppendJob j{k,    v,     dtype,  ldk,     ldv,  n_tokens, n_kv,  dim,
+                        slots, codes, params, n_pages, page, rotate != 0, k_hat, v_hat};
+  return kq::cache_append_launch(j, as_stream(stream));
+}
+
+int kronq_cache_attention(const void* q, int64_t ldq, int64_t n_tokens, int64_t n_heads,
+                          int64_t n_kv, int64_t dim, const uint32_t* codes, const uint32_t* params,
+                          int64_t n_pages, int64_t page, const int32_t* table, int64_t ldt,
+                          int64_t table_pages, const int32_t* lengths, int64_t n_seqs,
+                          const int32_t* starts, int64_t max_new, float scale, int rotate,
+                          void* out, int64_t ldo, void* ws, size_t ws_bytes, void* stream) {
+  kq::clear_error();
+  KQ_TRY(check_cache(codes, params, n_pages, page, n_kv, dim));
+  KQ_REQUIRE(n_heads >= 1 && n_heads % n_kv == 0 && n_heads <= 65535, KRONQ_ERR_SHAPE,
+             "n_heads must be a positive multiple of n_kv, at most 65535");
+  KQ_REQUIRE(n_tokens >= 0 && n_tokens <= (int64_t(1) << 31) / (n_heads * 4),
+             KRONQ_ERR_INVALID_ARG, "bad n_tokens");
+  KQ_REQUIRE(n_seqs >= 0 && n_seqs <= 65535, KRONQ_ERR_UNSUPPORTED, "n_seqs must be at most 65535");
+  if (n_tokens == 0 || n_seqs == 0) return KRONQ_OK;
+  KQ_REQUIRE(q && aligned(q, 16) && ldq % 8 == 0 && (n_tokens == 1 || ldq >= n_heads * dim),
+             KRONQ_ERR_INVALID_ARG,
+             "q must be 16-byte aligned with ldq >= n_heads * dim, divisible by 8");
+  KQ_REQUIRE(out && aligned(out, 2) && (n_tokens == 1 || ldo >= n_heads * dim),
+             KRONQ_ERR_INVALID_ARG, "out must be 2-byte aligned with ldo >= n_heads * dim");
+  KQ_REQUIRE(table && aligned(table, 4) && table_pages >= 1 && ldt >= table_pages &&
+                 table_pages <= ((int64_t(1) << 30) / page),
+             KRONQ_ERR_INVALID_ARG,
+             "table needs 1 <= table_pages <= ldt and table_pages * page <= 2^30");
+  KQ_REQUIRE(lengths && aligned(lengths, 4) && aligned(starts, 4), KRONQ_ERR_INVALID_ARG,
+             "lengths is NULL or misaligned");
+  KQ_REQUIRE(starts || n_tokens <= n_seqs, KRONQ_ERR_SHAPE,
+             "without starts there is one token per sequence");
+  KQ_REQUIRE(max_new >= 1 && max_new <= n_tokens, KRONQ_ERR_INVALID_ARG,
+             "1 <= max_new <= n_tokens");
+  KQ_TRY(check_ws(ws, ws_bytes, kq::attention_ws_bytes(n_heads, dim, n_tokens)));
+  const kq::AttentionJob j{q,      ldq,   n_tokens,    n_heads, n_kv,   dim,    codes,
+                           params, n_pages, page,      table,   ldt,    table_pages, lengths,
+                           n_seqs, starts, max_new,    scale,   rotate != 0, out, ldo};
+  return kq::cache_attention_launch(j, ws, as_stream(stream));
 }
 
 int kronq_layer_loss(const void* W, int w_dtype, int64_t ldw, const float* W_hat,

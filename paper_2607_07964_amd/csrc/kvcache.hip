@@ -1,0 +1,642 @@
+// Keys and values of a served model in a paged cache of 4-bit codes, and attention over it.
+//
+// A row (the key or the value of one token and kv head, dim values) is quantised on the min-max
+// grid of the weights, 16 levels: after an optional Hadamard transform r = H v / sqrt(dim) (which
+// spreads a strong channel over the row; queries take the same transform, so that products do not
+// change, and outputs its inverse, H again),
+//   scale = (max(0, r) - min(0, r)) / 15 rounded up to bf16 (at least 2^-100),
+//   zero = rint(-min(0, r) / scale), code = clamp(rint(r / scale) + zero, 0, 15).
+// Layout: codes [page][kv head][key, value][words of a page], eight codes to a word, low bits
+// first; a key row is dim / 8 consecutive words, value rows are interleaved four tokens at a time
+// ([token / 4][word][token % 4]) so that a lane's load brings it four tokens of its channels.
+// params [page][kv head][key, value][token]: scale (bf16, upper half) and zero (lower half).
+#include <cmath>
+
+#include "kq_common.hpp"
+#include "kq_fwht.hpp"
+
+namespace kq {
+namespace {
+
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint16_t f32_bf16(float v) {
+  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+}
+
+// ---- append --------------------------------------------------------------------------------------
+struct AppendArgs {
+  const void *k, *v;
+  int64_t ldk, ldv, n_tokens;
+  int n_kv, page_log;
+  int64_t n_slots;
+  const int64_t* slots;
+  uint32_t *codes, *params;
+  int rotate;
+  double norm;
+  float *k_hat, *v_hat;
+};
+
+// dim / 8 lanes take a row, eight values each. In fp64: the transform is exact to 2^-52, so that a
+// code depends on the row alone and not on the order of the sums; bound by the reads and writes of
+// the rows all the same.
+template <typename T, int DIM>
+__global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
+  constexpr int LPR = DIM / 8, RPW = 256 / LPR;  // lanes per row, rows per workgroup
+  const int l = threadIdx.x % LPR;
+  const int64_t row = int64_t(blockIdx.x) * RPW + threadIdx.x / LPR;  // token, head, key or value
+  const int64_t rows = A.n_tokens * A.n_kv * 2;
+  if (row >= rows) return;  // (whole groups of LPR lanes)
+  const int part = int(row & 1);
+  const int64_t th = row >> 1, token = th / A.n_kv;
+  const int head = int(th % A.n_kv);
+  const int64_t slot = A.slots[token];
+  if (slot < 0 || slot >= A.n_slots) return;
+  const T* src = static_cast<const T*>(part ? A.v : A.k) + token * (part ? A.ldv : A.ldk) +
+                 int64_t(head) * DIM + l * 8;
+  double r[8];
+  if constexpr (sizeof(T) == 2) {
+    const uint4 w = *reinterpret_cast<const uint4*>(src);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r[2 * i] = __uint_as_float(u[i] << 16);
+      r[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      const float4 w = *reinterpret_cast<const float4*>(src + i);
+      r[i] = w.x, r[i + 1] = w.y, r[i + 2] = w.z, r[i + 3] = w.w;
+    }
+  }
+  if (A.rotate) {
+#pragma unroll
+    for (int s = 1; s < 8; s <<= 1)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (!(i & s)) {
+          const double a = r[i], b = r[i + s];
+          r[i] = a + b, r[i + s] = a - b;
+        }
+#pragma unroll
+    for (int o = 1; o < LPR; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double p = __shfl_xor(r[i], o);
+        r[i] = (l & o) ? p - r[i] : r[i] + p;
+      }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] *= A.norm;
+  }
+  double lo = 0.0, hi = 0.0;
+  int bad = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo = fmin(lo, r[i]), hi = fmax(hi, r[i]);
+    bad |= !(fabs(r[i]) <= 3.0e38);  // NaN, infinities, and values whose grid bf16 cannot hold
+  }
+#pragma unroll
+  for (int o = 1; o < LPR; o <<= 1) {
+    lo = fmin(lo, __shfl_xor(lo, o)), hi = fmax(hi, __shfl_xor(hi, o));
+    bad |= __shfl_xor(bad, o);
+  }
+  const double wide = fmax((hi - lo) / 15.0, 0x1p-100);
+  // up to bf16: 45 of the 52 bits of the fraction go
+  const uint64_t up = (__builtin_bit_cast(uint64_t, wide) + ((uint64_t(1) << 45) - 1)) &
+                      ~((uint64_t(1) << 45) - 1);
+  const double scale = __builtin_bit_cast(double, up), inv = 1.0 / scale;
+  const double zero = fmin(rint(-lo / scale), 15.0);
+  uint32_t word = 0;
+  float hat[8];
+  // a row with a value that is not finite reads as NaN
+  const float sf = bad ? __uint_as_float(0x7FC00000u) : float(scale);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const double t = r[i] * inv;  // good to 2^-51: rint(t) is rint(r / scale) unless t is next to a
+    double n = rint(t);           // half, where the quotient itself decides
+    if (fabs(fabs(t - n) - 0.5) < 1e-12) n = rint(r[i] / scale);
+    const double c = bad ? 0.0 : fmin(fmax(n + zero, 0.0), 15.0);
+    word |= uint32_t(int(c)) << (4 * i);
+    hat[i] = sf * float(c - zero);
+  }
+  const int64_t p = slot >> A.page_log, off = slot & ((int64_t(1) << A.page_log) - 1);
+  const int64_t ph = (p * A.n_kv + head) * 2 + part;
+  const int64_t at = part ? ((off >> 2) * LPR + l) * 4 + (off & 3) : off * LPR + l;
+  A.codes[((ph << A.page_log) * LPR) + at] = word;
+  if (l == 0)
+    A.params[(ph << A.page_log) + off] = __float_as_uint(sf) | (bad ? 0u : uint32_t(int(zero)));
+  float* out = part ? A.v_hat : A.k_hat;
+  if (out) {
+    out += th * DIM + l * 8;
+    *reinterpret_cast<float4*>(out) = make_float4(hat[0], hat[1], hat[2], hat[3]);
+    *reinterpret_cast<float4*>(out + 4) = make_float4(hat[4], hat[5], hat[6], hat[7]);
+  }
+}
+
+// ---- attention -----------------------------------------------------------------------------------
+// For one sequence and kv head, the new tokens' queries of the heads that share it are rows: row
+// i G + g is token i, head g of G. A workgroup of four waves takes 16 MQ rows and a range of the
+// cached tokens, which its waves walk in turn, 32 tokens at a time, each with its own running
+// maximum and sums; they meet in LDS once at the end. One pass over the cache:
+//   scores   S[token][row] = K q on v_mfma_f32_16x16x32_f16, twice 16 tokens: a lane spreads the
+//            codes of its token and channels straight from the loaded words. A code left at bit 0
+//            or 4 of its half word is the subnormal fp16 c 2^-24 or c 2^-20, so a pair of codes
+//            costs one AND (and every second word a shift); the power of 16 between the two is
+//            inside q. S = s_t (sum c q - z_t sum q).
+//   weights  p = 2^(S - m) with m a reference that follows the running maximum only when that
+//            leaves it by more than 2^7, so that most tiles rescale nothing and compare without
+//            crossing lanes. The weight that meets the value codes is p s_t / sigma as fp16, sigma
+//            following the largest value scale the same way.
+//   outputs  O[row][channel] += (p s) c: the lane that held S for a row and four tokens of either
+//            half holds its weights for the same tokens as the A operand (the order of tokens in a
+//            sum is free), so nothing crosses lanes; sum (p s) z beside it.
+// fp16 for q (2^-11), for the weights (2^-11, and never coarser than 2^-25 of the largest value
+// scale); everything summed in fp32; outputs bf16.
+struct AttnArgs {
+  const uint16_t* q;
+  int64_t ldq, n_tokens;
+  int n_heads, n_kv, group;
+  const uint32_t *codes, *params;
+  int64_t n_pages;
+  int page_log;
+  const int* table;
+  int64_t ldt;
+  int table_pages;
+  const int* lengths;
+  const int* starts;  // null: token b is sequence b
+  float scale;        // of the scores, times log2(e)
+  int rotate;
+  int tiles, splits;
+  uint16_t* out;
+  int64_t ldo;
+  float *part, *ml;   // splits > 1: [split][token][head][dim], and maximum and sum
+};
+
+// lane + 64 e of a row of DIM = 64 or 128 values: H x / sqrt(DIM)
+template <int DIM>
+__device__ __forceinline__ void rotate_row(float (&x)[2], int lane) {
+  hadamard_lanes<2>(x, lane);
+  if constexpr (DIM == 128) {
+    const float a = x[0], b = x[1];
+    x[0] = a + b, x[1] = a - b;
+  }
+  x[0] *= DIM == 128 ? 0.08838834764831845f : 0.125f;
+  x[1] *= 0.08838834764831845f;
+}
+
+template <int DIM>
+__device__ __forceinline__ void store_row(uint16_t* o, float (&x)[2], int lane, int rotate) {
+  if (rotate) rotate_row<DIM>(x, lane);
+  o[lane] = f32_bf16(x[0]);
+  if constexpr (DIM == 128) o[lane + 64] = f32_bf16(x[1]);
+}
+
+__device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a),
+                                                __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+
+// what a wave loads of 32 tokens: codes and parameters of both halves of 16
+template <int NJ>
+struct KvTile {
+  uint32_t k[2][NJ], v[2][4], kp[2][4], vp[2][4];
+  int bad;  // halves on pages that do not exist
+};
+
+template <int DIM, int MQ>
+__global__ __launch_bounds__(256) void cache_attention(AttnArgs A) {
+  constexpr int NJ = DIM / 32;       // words of a key row a lane takes, matrix steps per score
+  constexpr int ND = DIM / 16;       // output blocks of 16 channels
+  constexpr int WPR = DIM / 8;       // words per row
+  constexpr int ROWS = 16 * MQ, LD = DIM + 4;
+  extern __shared__ __attribute__((aligned(16))) float sm[];  // [wave][row][LD], [wave][row][2]
+  float* sml = sm + 4 * ROWS * LD;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, g4 = lane >> 4;
+  const int b = blockIdx.z, h = blockIdx.y;
+  const int split = blockIdx.x % A.splits;
+  const int nt = int(A.n_tokens);
+  int q0 = b, q1 = b + 1;
+  if (A.starts) {
+    q0 = A.starts[b], q1 = A.starts[b + 1];
+    q0 = q0 < 0 ? 0 : q0 > nt ? nt : q0;
+    q1 = q1 < q0 ? q0 : q1 > nt ? nt : q1;
+  }
+  const int nq = q1 - q0, G = A.group, nrows = nq * G;
+  int len = A.lengths[b];
+  const int most = A.table_pages << A.page_log;
+  len = len < 0 ? 0 : len > most ? most : len;
+  const int* table = A.table + int64_t(b) * A.ldt;
+  const int page_mask = (1 << A.page_log) - 1;
+  // later rows see more tokens: they go first
+  const int tiles = (nrows + ROWS - 1) / ROWS;
+  for (int tile = tiles - 1 - int(blockIdx.x / A.splits); tile >= 0; tile -= A.tiles) {
+    const int row0 = tile * ROWS;
+    const int end_row = row0 + ROWS < nrows ? row0 + ROWS : nrows;
+    // tokens that the tile's first and last rows see
+    const int see0 = len - nq + row0 / G + 1, see1 = len - nq + (end_row - 1) / G + 1;
+    const int end = see1 > 0 ? see1 : 0;
+    int chunk = (end + A.splits - 1) / A.splits;
+    chunk = (chunk + 127) & ~127;
+    const int beg_t = split * chunk, end_t = beg_t + chunk < end ? beg_t + chunk : end;
+
+    // queries as the B operand: row n of each 16, channels 8 NJ g4 + 8 j + {0 4 1 5 2 6 3 7}, odd
+    // pairs divided by 16; the whole row by a power of two
+    u32x4_t qf[MQ][NJ];
+    float qsum[MQ], qs[MQ];
+    int see[MQ];
+#pragma unroll
+    for (int i = 0; i < MQ; ++i) {
+      const int row = row0 + 16 * i + n < nrows ? row0 + 16 * i + n : nrows - 1;
+      see[i] = len - nq + row / G + 1;
+      const uint16_t* src = A.q + int64_t(q0 + row / G) * A.ldq + int64_t(h * G + row % G) * DIM;
+      float x[8 * NJ];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const u32x4_t w = *reinterpret_cast<const u32x4_t*>(src + 8 * (NJ * g4 + j));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[8 * j + 2 * k] = __uint_as_float(w[k] << 16);
+          x[8 * j + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+        }
+      }
+      if (A.rotate) {
+        hadamard_reg<8 * NJ>(x);
+#pragma unroll
+        for (int o = 16; o < 64; o <<= 1)
+#pragma unroll
+          for (int k = 0; k < 8 * NJ; ++k) {
+            const float p = __shfl_xor(x[k], o);
+            x[k] = (lane & o) ? p - x[k] : x[k] + p;
+          }
+      }
+      float mx = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8 * NJ; ++k) mx = fmaxf(mx, fabsf(x[k]));
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const int e = int(__float_as_uint(mx) >> 23) - 127;
+      const int ue = mx > 0.f && e < 128 ? (e < -90 ? -90 : e) - 5 : 0;  // largest to [2^5, 2^6)
+      const float up = __uint_as_float(uint32_t(127 - ue) << 23);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        u32x4_t f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float lo = x[8 * j + k] * up, hi = x[8 * j + k + 4] * up;
+          f16x2_t p = {_Float16(lo), _Float16(hi)};
+          sum += float(p[0]) + float(p[1]);
+          if (k & 1) p *= f16x2_t{_Float16(0.0625f), _Float16(0.0625f)};
+          f[k] = __builtin_bit_cast(uint32_t, p);
+        }
+        qf[i][j] = f;
+      }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      qsum[i] = sum * 0x1p-24f;
+      qs[i] = A.scale * __uint_as_float(uint32_t(127 + ue) << 23) * 0x1p24f;
+      if (A.rotate) qs[i] *= DIM == 128 ? 0.08838834764831845f : 0.125f;
+    }
+
+    f32x4_t acc[MQ][ND] = {};
+    float m[MQ], l[MQ], zs[MQ], sigma = 0.f, sinv = 0.f;
+#pragma unroll
+    for (int i = 0; i < MQ; ++i) m[i] = -1e30f, l[i] = 0.f, zs[i] = 0.f;
+
+    auto load = [&](KvTile<NJ>& T, int t0) {
+      T.bad = 0;
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        int t = t0 + 16 * f;
+        t = t < end ? t : (end - 1) & ~15;  // past the end: the last tokens again, masked below
+        int p = table[t >> A.page_log];
+        if (p < 0 || p >= A.n_pages) p = 0, T.bad |= 1 << f;
+        const int off = t & page_mask;
+        const int64_t ph = (int64_t(p) * A.n_kv + h) * 2;
+        const uint32_t* kc = A.codes + ((ph << A.page_log) + off + n) * WPR + g4 * NJ;
+        const uint32_t* vc = A.codes + (((ph + 1) << A.page_log) + off) * WPR +
+                             (g4 * WPR + (n & (WPR - 1))) * 4;
+        const uint32_t* pp = A.params + (ph << A.page_log) + off + 4 * g4;
+        if constexpr (NJ == 4) {
+          const uint4 w = *reinterpret_cast<const uint4*>(kc);
+          T.k[f][0] = w.x, T.k[f][1] = w.y, T.k[f][2] = w.z, T.k[f][3] = w.w;
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(kc);
+          T.k[f][0] = w.x, T.k[f][1] = w.y;
+        }
+        const uint4 v = *reinterpret_cast<const uint4*>(vc);
+        T.v[f][0] = v.x, T.v[f][1] = v.y, T.v[f][2] = v.z, T.v[f][3] = v.w;
+        const uint4 a = *reinterpret_cast<const uint4*>(pp);
+        T.kp[f][0] = a.x, T.kp[f][1] = a.y, T.kp[f][2] = a.z, T.kp[f][3] = a.w;
+        const uint4 c = *reinterpret_cast<const uint4*>(pp + (1 << A.page_log));
+        T.vp[f][0] = c.x, T.vp[f][1] = c.y, T.vp[f][2] = c.z, T.vp[f][3] = c.w;
+      }
+    };
+
+    auto work = [&](const KvTile<NJ>& T, int t0) {
+      f32x4_t s[MQ][2] = {};
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const uint32_t w = T.k[f][j], w8 = w >> 8;
+          const u32x4_t a = {w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u};
+#pragma unroll
+          for (int i = 0; i < MQ; ++i) s[i][f] = mfma16(a, qf[i][j], s[i][f]);
+        }
+      // scales and zeros of this lane's tokens 16 f + 4 g4 + r
+      float ks[2][4], kz[2][4], vs[2][4], vz[2][4], svm = 0.f;
+      const bool cut = t0 + 32 > end_t || T.bad;  // (uniform)
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          ks[f][r] = __uint_as_float(T.kp[f][r] & 0xFFFF0000u), kz[f][r] = float(T.kp[f][r] & 0xFFu);
+          vs[f][r] = __uint_as_float(T.vp[f][r] & 0xFFFF0000u), vz[f][r] = float(T.vp[f][r] & 0xFFu);
+          if (cut && (t0 + 16 * f + 4 * g4 + r >= end_t || (T.bad >> f & 1)))
+            vs[f][r] = 0.f, vz[f][r] = 0.f;  // (whatever stands there counts for nothing)
+          svm = fmaxf(svm, vs[f][r]);
+        }
+      const bool mask = cut || t0 + 32 > see0;
+      bool up = svm > 128.f * sigma;
+      float top[MQ];
+#pragma unroll
+      for (int i = 0; i < MQ; ++i) {
+        top[i] = -INFINITY;
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float v = fmaf(-kz[f][r], qsum[i], s[i][f][r]) * (ks[f][r] * qs[i]);
+            if (mask) {
+              const int t = t0 + 16 * f + 4 * g4 + r;
+              if (t >= see[i] || t >= end_t || (T.bad >> f & 1)) v = -INFINITY;
+            }
+            s[i][f][r] = v;
+            top[i] = fmaxf(top[i], v);
+          }
+        up |= top[i] > m[i] + 7.f;
+      }
+      if (__any(up)) {  // new references
+        float sn = svm;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) sn = fmaxf(sn, __shfl_xor(sn, o));
+        sn = fmaxf(sn, sigma);
+        const float fs = sn > 0.f ? sigma / sn : 0.f;
+        sigma = sn;
+        sinv = sn > 0.f ? 1.f / sn : 0.f;
+#pragma unroll
+        for (int i = 0; i < MQ; ++i) {
+          float t = fmaxf(top[i], __shfl_xor(top[i], 16));
+          t = fmaxf(t, __shfl_xor(t, 32));
+          const float mn = fmaxf(m[i], t), fm = exp2f(m[i] - mn), fo = fm * fs;
+          m[i] = mn;
+          l[i] *= fm, zs[i] *= fo;
+          float fr[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) fr[r] = __shfl(fo, 4 * g4 + r);
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][d][r] *= fr[r];
+        }
+      }
+      u32x4_t pf[MQ];
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) vs[f][r] *= sinv;
+#pragma unroll
+      for (int i = 0; i < MQ; ++i)
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+          for (int r = 0; r < 4; r += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(s[i][f][r] - m[i]);
+            const float p1 = __builtin_amdgcn_exp2f(s[i][f][r + 1] - m[i]);
+            l[i] += p0 + p1;
+            float w0 = p0 * vs[f][r], w1 = p1 * vs[f][r + 1];
+            if (mask) {  // a hidden token's value may read as NaN
+              if (s[i][f][r] == -INFINITY) w0 = 0.f;
+              if (s[i][f][r + 1] == -INFINITY) w1 = 0.f;
+            }
+            zs[i] = fmaf(w0, vz[f][r], zs[i]);
+            zs[i] = fmaf(w1, vz[f][r + 1], zs[i]);
+            pf[i][2 * f + (r >> 1)] =
+                __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{w0, w1}, f16x2_t));
+          }
+      // value codes: channel 8 n + d, pairs of tokens
+      if constexpr (DIM == 128) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {  // low and high halves of the words: channels 0-3 and 4-7
+          u32x4_t w, w8;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            w[k] = __builtin_amdgcn_perm(T.v[k >> 1][2 * (k & 1) + 1], T.v[k >> 1][2 * (k & 1)],
+                                         x ? 0x07060302u : 0x05040100u);
+            w8[k] = w[k] >> 8;
+          }
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const u32x4_t bv = (d & 2 ? w8 : w) & (d & 1 ? 0x00F000F0u : 0x000F000Fu);
+#pragma unroll
+            for (int i = 0; i < MQ; ++i) acc[i][4 * x + d] = mfma16(pf[i], bv, acc[i][4 * x + d]);
+          }
+        }
+      } else {  // lanes n and n + 8 share a word: channels 0-3 and 4-7 of it
+        const uint32_t sel = n < 8 ? 0x05040100u : 0x07060302u;
+        u32x4_t w, w8;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          w[k] = __builtin_amdgcn_perm(T.v[k >> 1][2 * (k & 1) + 1], T.v[k >> 1][2 * (k & 1)], sel);
+          w8[k] = w[k] >> 8;
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const u32x4_t bv = (d & 2 ? w8 : w) & (d & 1 ? 0x00F000F0u : 0x000F000Fu);
+#pragma unroll
+          for (int i = 0; i < MQ; ++i) acc[i][d] = mfma16(pf[i], bv, acc[i][d]);
+        }
+      }
+    };
+
+    // this wave's tiles of 32 tokens, the next one loaded meanwhile
+    if (beg_t + 32 * wave < end_t) {
+      KvTile<NJ> T[2];
+      load(T[0], beg_t + 32 * wave);
+      for (int t0 = beg_t + 32 * wave;;) {
+        const int t1 = t0 + 128;
+        if (t1 < end_t) load(T[1], t1);
+        work(T[0], t0);
+        if (t1 >= end_t) break;
+        t0 = t1 + 128;
+        if (t0 < end_t) load(T[0], t0);
+        work(T[1], t1);
+        if (t0 >= end_t) break;
+      }
+    }
+
+    // the waves' parts to LDS
+#pragma unroll
+    for (int i = 0; i < MQ; ++i) {
+      l[i] += __shfl_xor(l[i], 16);
+      l[i] += __shfl_xor(l[i], 32);
+      zs[i] += __shfl_xor(zs[i], 16);
+      zs[i] += __shfl_xor(zs[i], 32);
+      float* o = sm + (wave * ROWS + 16 * i) * LD;
+      if (g4 == 0) {
+        sml[(wave * ROWS + 16 * i + n) * 2] = m[i];
+        sml[(wave * ROWS + 16 * i + n) * 2 + 1] = l[i];
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float z = __shfl(zs[i], 4 * g4 + r);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const float v = sigma * (acc[i][d][r] * (d & 1 ? 0x1p20f : 0x1p24f) - z);
+          const int ch = DIM == 128 ? 8 * n + d : 8 * (n & 7) + 4 * (n >> 3) + d;
+          o[(4 * g4 + r) * LD + ch] = v;
+        }
+      }
+    }
+    __syncthreads();
+    for (int row = wave; row < end_row - row0; row += 4) {
+      float mm[4], mx = -INFINITY, sum = 0.f, x[2] = {};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) mm[w] = sml[(w * ROWS + row) * 2], mx = fmaxf(mx, mm[w]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = exp2f(mm[w] - mx);
+        sum += f * sml[(w * ROWS + row) * 2 + 1];
+        x[0] += f * sm[(w * ROWS + row) * LD + lane];
+        if constexpr (DIM == 128) x[1] += f * sm[(w * ROWS + row) * LD + lane + 64];
+      }
+      const int64_t tok = q0 + (row0 + row) / G;
+      const int head = h * G + (row0 + row) % G;
+      if (A.splits > 1) {
+        const int64_t at = (int64_t(split) * A.n_tokens + tok) * A.n_heads + head;
+        A.part[at * DIM + lane] = x[0];
+        if constexpr (DIM == 128) A.part[at * DIM + lane + 64] = x[1];
+        if (lane == 0) A.ml[2 * at] = mx, A.ml[2 * at + 1] = sum;
+      } else {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;  // a row that sees nothing: zeros
+        x[0] *= inv, x[1] *= inv;
+        store_row<DIM>(A.out + tok * A.ldo + int64_t(head) * DIM, x, lane, A.rotate);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// the splits of a row (a wave each)
+template <int DIM>
+__global__ __launch_bounds__(256) void attention_join(AttnArgs A, int n_seqs) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6), rows = A.n_tokens * A.n_heads;
+  if (row >= rows) return;
+  const int64_t tok = row / A.n_heads;
+  if (A.starts) {  // tokens of no sequence were not computed
+    bool in = false;
+    for (int b = lane; b < n_seqs; b += 64) in |= tok >= A.starts[b] && tok < A.starts[b + 1];
+    if (!__any(in)) return;
+  } else if (tok >= n_seqs) {
+    return;
+  }
+  float mx = -INFINITY;
+  for (int s = 0; s < A.splits; ++s) mx = fmaxf(mx, A.ml[2 * (s * rows + row)]);
+  float x[2] = {}, sum = 0.f;
+  for (int s = 0; s < A.splits; ++s) {
+    const int64_t at = s * rows + row;
+    const float f = exp2f(A.ml[2 * at] - mx);
+    sum += f * A.ml[2 * at + 1];
+    x[0] += f * A.part[at * DIM + lane];
+    if constexpr (DIM == 128) x[1] += f * A.part[at * DIM + lane + 64];
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  x[0] *= inv, x[1] *= inv;
+  store_row<DIM>(A.out + tok * A.ldo + (row % A.n_heads) * DIM, x, lane, A.rotate);
+}
+
+// ---- plan and launches ---------------------------------------------------------------------------
+constexpr int64_t MAX_SPLITS = 32, SPLIT_ROWS = 131072;
+
+// rows of partial outputs that the workspace holds
+int64_t split_rows(int64_t rows) {
+  return rows * MAX_SPLITS < SPLIT_ROWS + rows ? rows * MAX_SPLITS : SPLIT_ROWS + rows;
+}
+
+template <int DIM, int MQ>
+int launch_attention(const AttnArgs& a, int64_t n_seqs, hipStream_t s) {
+  const size_t lds = size_t(4) * 16 * MQ * (DIM + 4 + 2) * sizeof(float);
+  const dim3 grid(static_cast<unsigned>(a.tiles * a.splits), static_cast<unsigned>(a.n_kv),
+                  static_cast<unsigned>(n_seqs));
+  KQ_TRY(launch("cache_attention", cache_attention<DIM, MQ>, grid, dim3(256), lds, s, a));
+  if (a.splits == 1) return KRONQ_OK;
+  return launch("attention_join", attention_join<DIM>,
+                dim3(static_cast<unsigned>(cdiv(a.n_tokens * a.n_heads, 4))), dim3(256), 0, s, a,
+                int(n_seqs));
+}
+
+}  // namespace
+
+int cache_append_launch(const AppendJob& j, hipStream_t s) {
+  AppendArgs a{};
+  a.k = j.k, a.v = j.v, a.ldk = j.ldk, a.ldv = j.ldv, a.n_tokens = j.n_tokens;
+  a.n_kv = int(j.n_kv), a.page_log = __builtin_ctzll(uint64_t(j.page));
+  a.n_slots = j.n_pages * j.page, a.slots = j.slots, a.codes = j.codes, a.params = j.params;
+  a.rotate = j.rotate, a.norm = 1.0 / std::sqrt(double(j.dim)), a.k_hat = j.k_hat, a.v_hat = j.v_hat;
+  const dim3 grid(static_cast<unsigned>(cdiv(j.n_tokens * j.n_kv * 2, 2048 / j.dim)));
+  const bool half = j.dtype == KRONQ_BF16;
+  if (j.dim == 128)
+    return half ? launch("cache_append", cache_append<uint16_t, 128>, grid, dim3(256), 0, s, a)
+                : launch("cache_append", cache_append<float, 128>, grid, dim3(256), 0, s, a);
+  return half ? launch("cache_append", cache_append<uint16_t, 64>, grid, dim3(256), 0, s, a)
+              : launch("cache_append", cache_append<float, 64>, grid, dim3(256), 0, s, a);
+}
+
+size_t attention_ws_bytes(int64_t n_heads, int64_t dim, int64_t n_tokens) {
+  if (n_heads <= 0 || dim <= 0 || n_tokens <= 0) return 0;
+  const size_t rows = size_t(split_rows(n_heads * n_tokens));
+  return align256(rows * size_t(dim) * 4) + align256(rows * 8);
+}
+
+int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {
+  AttnArgs a{};
+  a.q = static_cast<const uint16_t*>(j.q), a.ldq = j.ldq, a.n_tokens = j.n_tokens;
+  a.n_heads = int(j.n_heads), a.n_kv = int(j.n_kv), a.group = int(j.n_heads / j.n_kv);
+  a.codes = j.codes, a.params = j.params, a.n_pages = j.n_pages;
+  a.page_log = __builtin_ctzll(uint64_t(j.page));
+  a.table = j.table, a.ldt = j.ldt, a.table_pages = int(j.table_pages), a.lengths = j.lengths;
+  a.starts = j.starts, a.scale = j.scale * 1.4426950408889634f, a.rotate = j.rotate;
+  a.out = static_cast<uint16_t*>(j.out), a.ldo = j.ldo;
+  const int64_t rows = j.max_new * a.group;  // of a sequence and kv head
+  const int mq = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  a.tiles = int(cdiv(rows, 16 * mq));
+  const int64_t wgs = a.tiles * j.n_kv * j.n_seqs, all = j.n_tokens * j.n_heads;
+  int64_t splits = cdiv(1024, wgs);
+  const int64_t useful = cdiv(j.table_pages * j.page, 256);
+  splits = splits < useful ? splits : useful;
+  splits = splits < MAX_SPLITS ? splits : MAX_SPLITS;
+  if (splits * all > split_rows(all)) splits = split_rows(all) / all;
+  a.splits = int(splits < 1 ? 1 : splits);
+  Carver cv(ws);
+  const size_t cap = size_t(split_rows(all));
+  a.part = cv.take<float>(cap * size_t(j.dim));
+  a.ml = cv.take<float>(cap * 2);
+  if (j.dim == 128)
+    return mq == 1   ? launch_attention<128, 1>(a, j.n_seqs, s)
+           : mq == 2 ? launch_attention<128, 2>(a, j.n_seqs, s)
+                     : launch_attention<128, 4>(a, j.n_seqs, s);
+  return mq == 1   ? launch_attention<64, 1>(a, j.n_seqs, s)
+         : mq == 2 ? launch_attention<64, 2>(a, j.n_seqs, s)
+                   : launch_attention<64, 4>(a, j.n_seqs, s);
+}
+
+}  // namespace kq

@@ -702,12 +702,12 @@ size_t online_ws_bytes(int64_t d_out, int64_t d_in, int64_t batch) {
          2 * align256(size_t(batch) * size_t(d_in / 128) * sizeof(float)) + 256;
 }
 
-int online_matvec_launch(const uint32_t* packed, int64_t ldp, const float* scales,
-                         const float* zeros, int64_t ldsz, int bits, int group, int64_t d_out,
-                         int64_t d_in, const float* mul_in, const float* mul_out,
-                         const float* q28_in, const float* q28_out, int flags, const void* x,
-                         int x_dtype, int64_t ldx, int64_t batch, float* y, int64_t ldy, void* ws,
-                         hipStream_t s) {
+// y' = W_hat' V S_X^-1 x for the rows of x; *y_rot receives y' (fp32 [batch x d_out], in ws)
+int online_product_launch(const uint32_t* packed, int64_t ldp, const float* scales,
+                          const float* zeros, int64_t ldsz, int bits, int group, int64_t d_out,
+                          int64_t d_in, const float* mul_in, const float* q28_in, int flags,
+                          const void* x, int x_dtype, int64_t ldx, int64_t batch, void* ws,
+                          float** y_rot, hipStream_t s) {
   Carver cv(ws);
   float* xr = cv.take<float>(size_t(batch) * size_t(d_in));
   float* yr = cv.take<float>(size_t(batch) * size_t(d_out));
@@ -732,6 +732,19 @@ int online_matvec_launch(const uint32_t* packed, int64_t ldp, const float* scale
          : bits == 4 ? KQ_GEMV_BITS(4)
                      : KQ_GEMV_BITS(8));
 #undef KQ_GEMV_BITS
+  *y_rot = yr;
+  return KRONQ_OK;
+}
+
+int online_matvec_launch(const uint32_t* packed, int64_t ldp, const float* scales,
+                         const float* zeros, int64_t ldsz, int bits, int group, int64_t d_out,
+                         int64_t d_in, const float* mul_in, const float* mul_out,
+                         const float* q28_in, const float* q28_out, int flags, const void* x,
+                         int x_dtype, int64_t ldx, int64_t batch, float* y, int64_t ldy, void* ws,
+                         hipStream_t s) {
+  float* yr;
+  KQ_TRY(online_product_launch(packed, ldp, scales, zeros, ldsz, bits, group, d_out, d_in, mul_in,
+                               q28_in, flags, x, x_dtype, ldx, batch, ws, &yr, s));
   // y = S_G^-1 U^T y'
   return seg_transform_launch(yr, KRONQ_FP32, d_out, y, ldy, batch, d_out, nullptr, mul_out,
                               (flags & KRONQ_ROT_OUT) != 0, q28_out, true, s);

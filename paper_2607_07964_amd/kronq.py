@@ -23,7 +23,8 @@ HX_ONLY, SX_GIVEN, HG_DIAG, SG_GIVEN = 32, 64, 128, 256
 BIIP = RESCALE_IN | RESCALE_OUT | ROT_IN | ROT_OUT
 OP_COV, OP_ROTATE, OP_CHOL, OP_OBS, OP_LOSS = 1, 2, 3, 4, 5
 OP_CROSS, OP_ROTATE_DRIFT, OP_GPTAQ, OP_OBS_DRIFT, OP_ONLINE = 6, 7, 8, 9, 10
-OP_STATS, OP_EIGH, OP_PROXY, OP_COV_DIAG = 11, 12, 13, 14
+OP_STATS, OP_EIGH, OP_PROXY, OP_COV_DIAG, OP_LINEAR, OP_ATTENTION = 11, 12, 13, 14, 15, 16
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 MAX_ALPHAS = 16
 ERRORS = {0: "OK", -1: "INVALID_ARG", -2: "SHAPE", -3: "NOT_PD", -4: "HIP", -5: "WORKSPACE",
           -6: "UNSUPPORTED"}
@@ -37,6 +38,8 @@ EXPORTS = (
     "kronq_online_factors", "kronq_online_matvec", "kronq_matrix_stats", "kronq_eigh",
     "kronq_proxy_loss_factors", "kronq_accumulate_cov_limited", "kronq_cov_diag",
     "kronq_cov_diag_noalloc", "kronq_probe_mfma_bf16", "kronq_accumulate_cross_limited",
+    "kronq_online_linear", "kronq_online_grouped", "kronq_grouped_workspace_bytes",
+    "kronq_cache_append", "kronq_cache_attention",
 )
 
 
@@ -79,6 +82,15 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "kronq_online_factors": (I, [P, P, I64, P, P]),
         "kronq_online_matvec": (I, [P, I64, P, P, I64, I, I, I64, I64, P, P, P, P, I, P, I, I64,
                                     I64, P, I64, P, SZ, P]),
+        "kronq_online_linear": (I, [P, I64, P, P, I64, I, I, I64, I64, P, P, P, P, I, P, I, I64,
+                                    I64, P, I, P, I64, P, I, I64, P, SZ, P]),
+        "kronq_online_grouped": (I, [P, I64, P, P, I64, I, I, I64, I64, P, P, P, P, I, P, I, I64,
+                                     I64, P, I64, P, I, P, I64, P, I, I64, P, SZ, P]),
+        "kronq_grouped_workspace_bytes": (SZ, [I64, I64, I64, I64]),
+        "kronq_cache_append": (I, [P, P, I, I64, I64, I64, I64, I64, P, P, P, I64, I64, I, P, P,
+                                   P]),
+        "kronq_cache_attention": (I, [P, I64, I64, I64, I64, I64, P, P, I64, I64, P, I64, I64, P,
+                                      I64, P, I64, F, I, P, I64, P, SZ, P]),
         "kronq_matrix_stats": (I, [P, I, I64, I64, I64, P, P, SZ, P]),
         "kronq_eigh": (I, [P, I64, I64, I, P, P, I64, P, P, SZ, P]),
         "kronq_proxy_loss_factors": (I, [P, I64, I64, P, I, I64, I64, P, I64, P, I64, P, I, P, P,
@@ -407,6 +419,229 @@ def kronq_online_matvec(packed: torch.Tensor, scales: torch.Tensor, zeros: torch
         _dtype_code(x), _ld(x), batch, _ptr(y), _ld(y), _ptr(ws), ws.numel(), _stream(x.device))
     _check(rc, "kronq_online_matvec")
     return y
+
+
+def _same_device(*ts):
+    """The one device of the tensors given (None: absent)."""
+    dev = None
+    for t in ts:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("libkronq works on device tensors only")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+    return dev
+
+
+def _typed(t: Optional[torch.Tensor], dtype, shape, name: str):
+    """``t`` (or None) with this dtype and these contiguous elements."""
+    if t is None:
+        return
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, "
+                         f"not {t.dtype} {tuple(t.shape)}")
+
+
+def _served(func, packed, scales, zeros, bits, group, d_in, mul_in, mul_out, q28_in, q28_out, x,
+            y, bias, act, residual, flags, ws, out_dtype, offsets, n_experts):
+    """Checks and call shared by kronq_online_linear and kronq_online_grouped."""
+    lib = load()
+    dev = _same_device(x, packed, scales, zeros, mul_in, mul_out, q28_in, q28_out, y, bias,
+                       residual, ws, offsets)
+    if act not in ACTS:
+        raise ValueError(f"act must be one of {sorted(ACTS)}, not {act!r}")
+    lead = () if offsets is None else (n_experts,)
+    w_rows = packed.shape[0]
+    if w_rows % n_experts:
+        raise ValueError(f"{w_rows} rows of codes for {n_experts} experts")
+    d_out = w_rows // n_experts
+    if packed.dtype not in (torch.int32, torch.uint32) or packed.shape[1] * 32 < d_in * bits:
+        raise ValueError("packed must be 32-bit words of d_in * bits / 32 columns")
+    for t, name in ((scales, "scales"), (zeros, "zeros")):
+        if t.dtype != torch.float32 or t.dim() != 2 or t.shape[0] != w_rows or \
+                t.shape[1] * group < d_in:
+            raise ValueError(f"{name} must be float32 [{w_rows} x d_in / group]")
+    if _ld(scales) != _ld(zeros):
+        raise ValueError("scales and zeros must have the same row stride")
+    _typed(mul_in, torch.float32, lead + (d_in,), "mul_in")
+    _typed(mul_out, torch.float32, lead + (d_out,), "mul_out")
+    _typed(bias, torch.float32, lead + (d_out,), "bias")
+    _typed(q28_in, torch.float32, lead + (28, 28), "q28_in")
+    _typed(q28_out, torch.float32, lead + (28, 28), "q28_out")
+    if x.dim() != 2 or x.shape[1] != d_in:
+        raise ValueError(f"x must be [rows x {d_in}]")
+    n = x.shape[0]
+    if y is None:
+        y = torch.empty(n, d_out, dtype=out_dtype or x.dtype, device=dev)
+    elif out_dtype not in (None, y.dtype):
+        raise ValueError(f"y is {y.dtype}, out_dtype {out_dtype}")
+    if y.dim() != 2 or y.shape[0] != n or y.shape[1] != d_out:
+        raise ValueError(f"y must be [{n} x {d_out}]")
+    if residual is not None and (residual.shape != y.shape or residual.dtype != y.dtype):
+        raise ValueError("residual must have y's shape and dtype")
+    # (a single row has any row stride)
+    ldx = _ld(x) if n > 1 else -(-d_in // 8) * 8
+    ldy = _ld(y) if n > 1 else d_out
+    ldr = 0 if residual is None else _ld(residual) if n > 1 else d_out
+    with torch.cuda.device(dev):
+        if ws is None:
+            need = lib.kronq_workspace_bytes(OP_LINEAR, d_out, d_in, n) if offsets is None else \
+                lib.kronq_grouped_workspace_bytes(d_out, d_in, n, n_experts)
+            ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        head = (packed.data_ptr(), _ld(packed), scales.data_ptr(), zeros.data_ptr(), _ld(scales),
+                bits, group, d_out, d_in, _ptr(mul_in), _ptr(mul_out), _ptr(q28_in), _ptr(q28_out),
+                flags, x.data_ptr(), _dtype_code(x), ldx, n)
+        tail = (_ptr(bias), ACTS[act], _ptr(residual), ldr, y.data_ptr(), _dtype_code(y), ldy,
+                ws.data_ptr(), ws.numel() * ws.element_size(), _stream(dev))
+        if offsets is None:
+            rc = lib.kronq_online_linear(*head, *tail)
+        else:
+            rc = lib.kronq_online_grouped(*head, offsets.data_ptr(), n_experts, *tail)
+    _check(rc, func)
+    return y
+
+
+def kronq_online_linear(packed: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor,
+                        bits: int, group: int, d_in: int, mul_in: Optional[torch.Tensor],
+                        mul_out: Optional[torch.Tensor], q28_in: Optional[torch.Tensor],
+                        q28_out: Optional[torch.Tensor], x: torch.Tensor,
+                        y: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                        act: str = "none", residual: Optional[torch.Tensor] = None,
+                        flags: int = BIIP, ws: Optional[torch.Tensor] = None,
+                        out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """y = act(diag(mul_out) T_out W_hat' T_in diag(mul_in) x + bias) + residual for the rows of x
+    [n x d_in]; y (bf16 or fp32) defaults to x's dtype or ``out_dtype``."""
+    return _served("kronq_online_linear", packed, scales, zeros, bits, group, d_in, mul_in,
+                   mul_out, q28_in, q28_out, x, y, bias, act, residual, flags, ws, out_dtype, None,
+                   1)
+
+
+def kronq_online_grouped(packed: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor,
+                         bits: int, group: int, d_in: int, mul_in: Optional[torch.Tensor],
+                         mul_out: Optional[torch.Tensor], q28_in: Optional[torch.Tensor],
+                         q28_out: Optional[torch.Tensor], x: torch.Tensor, offsets: torch.Tensor,
+                         y: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                         act: str = "none", residual: Optional[torch.Tensor] = None,
+                         flags: int = BIIP, ws: Optional[torch.Tensor] = None,
+                         out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """kronq_online_linear with a layer per expert, for rows sorted by expert: rows offsets[e] to
+    offsets[e + 1] - 1 (int32, on the device) belong to expert e; other rows of y stay as they are
+    (zeros where y is made here). Per-expert tensors have the experts first; packed, scales and
+    zeros are [experts * d_out x ...]."""
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous():
+        raise ValueError("offsets must be a contiguous int32 vector")
+    n_experts = offsets.numel() - 1
+    if n_experts < 1:
+        raise ValueError("offsets must hold at least two values")
+    if y is None:
+        y = torch.zeros(x.shape[0], packed.shape[0] // n_experts, dtype=out_dtype or x.dtype,
+                        device=x.device)
+    return _served("kronq_online_grouped", packed, scales, zeros, bits, group, d_in, mul_in,
+                   mul_out, q28_in, q28_out, x, y, bias, act, residual, flags, ws, out_dtype,
+                   offsets, n_experts)
+
+
+def _cache_sizes(codes: torch.Tensor, params: torch.Tensor):
+    """(pages, kv heads, page, dim) of a cache."""
+    if params.dim() != 4 or codes.dim() != 4 or codes.shape[:3] != params.shape[:3] or \
+            params.shape[2] != 2:
+        raise ValueError("the cache is codes [pages, kv heads, 2, page * dim / 8] and "
+                         "params [pages, kv heads, 2, page]")
+    for t in (codes, params):
+        if t.dtype not in (torch.int32, torch.uint32) or not t.is_contiguous():
+            raise ValueError("codes and params must be contiguous 32-bit words")
+    page = params.shape[3]
+    if page < 1 or codes.shape[3] * 8 % page:
+        raise ValueError("codes and params differ in their page")
+    return params.shape[0], params.shape[1], page, codes.shape[3] * 8 // page
+
+
+def _token_stride(t: torch.Tensor, heads: int, dim: int, name: str) -> int:
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"{name} must be [tokens, {heads}, {dim}]")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"the heads of a token of {name} must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+def kronq_cache_empty(pages: int, kv_heads: int, dim: int, page: int = 64, device="cuda"):
+    """(codes, params) of an empty 4-bit cache."""
+    return (torch.zeros(pages, kv_heads, 2, page * dim // 8, dtype=torch.int32, device=device),
+            torch.zeros(pages, kv_heads, 2, page, dtype=torch.int32, device=device))
+
+
+def kronq_cache_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, codes: torch.Tensor,
+                       params: torch.Tensor, rotate: bool = True,
+                       k_hat: Optional[torch.Tensor] = None,
+                       v_hat: Optional[torch.Tensor] = None) -> None:
+    """Write keys and values [tokens, kv heads, dim] (bf16 or fp32) at slots (int64; page * place
+    index, negative: left out) of the 4-bit cache; k_hat and v_hat (fp32) receive what it holds."""
+    dev = _same_device(k, v, slots, codes, params, k_hat, v_hat)
+    pages, kv, page, dim = _cache_sizes(codes, params)
+    n = k.shape[0]
+    ldk, ldv = _token_stride(k, kv, dim, "k"), _token_stride(v, kv, dim, "v")
+    if v.shape[0] != n or v.dtype != k.dtype:
+        raise ValueError("k and v must have the same tokens and dtype")
+    _typed(slots, torch.int64, (n,), "slots")
+    _typed(k_hat, torch.float32, (n, kv, dim), "k_hat")
+    _typed(v_hat, torch.float32, (n, kv, dim), "v_hat")
+    with torch.cuda.device(dev):
+        rc = load().kronq_cache_append(k.data_ptr(), v.data_ptr(), _dtype_code(k), ldk, ldv, n, kv,
+                                       dim, slots.data_ptr(), codes.data_ptr(), params.data_ptr(),
+                                       pages, page, int(rotate), _ptr(k_hat), _ptr(v_hat),
+                                       _stream(dev))
+    _check(rc, "kronq_cache_append")
+
+
+def kronq_cache_attention(q: torch.Tensor, codes: torch.Tensor, params: torch.Tensor,
+                          table: torch.Tensor, lengths: torch.Tensor,
+                          starts: Optional[torch.Tensor] = None, max_new: Optional[int] = None,
+                          scale: Optional[float] = None, rotate: bool = True,
+                          out: Optional[torch.Tensor] = None,
+                          ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new tokens q [tokens, heads, dim] (bf16) over the 4-bit cache. Tokens
+    starts[b] to starts[b + 1] - 1 are the last of the lengths[b] cached tokens of sequence b (no
+    starts: one each), whose pages table[b] names. ``max_new`` (default: all tokens, or 1 without
+    starts) is about the most new tokens of a sequence; ``scale`` defaults to dim ** -0.5."""
+    lib = load()
+    dev = _same_device(q, codes, params, table, lengths, starts, out, ws)
+    pages, kv, page, dim = _cache_sizes(codes, params)
+    n, heads = q.shape[0], q.shape[1]
+    ldq = _token_stride(q, heads, dim, "q")
+    if q.dtype != torch.bfloat16:
+        raise ValueError("q must be bfloat16")
+    if out is None:
+        out = torch.empty(n, heads, dim, dtype=torch.bfloat16, device=dev) if starts is None else \
+            torch.zeros(n, heads, dim, dtype=torch.bfloat16, device=dev)
+    if out.dtype != torch.bfloat16 or out.shape[0] != n:
+        raise ValueError("out must be bfloat16 with q's shape")
+    ldo = _token_stride(out, heads, dim, "out")
+    seqs = table.shape[0]
+    if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1
+                                                         and table.stride(1) != 1):
+        raise ValueError("table must be int32 [sequences x pages]")
+    _typed(lengths, torch.int32, (seqs,), "lengths")
+    _typed(starts, torch.int32, (seqs + 1,), "starts")
+    if starts is None and n != seqs:
+        raise ValueError("without starts there is one token per sequence")
+    if n == 0 or seqs == 0:
+        return out
+    most = max_new if max_new is not None else 1 if starts is None else n
+    ldt = table.stride(0) if seqs > 1 else table.shape[1]
+    with torch.cuda.device(dev):
+        if ws is None:
+            ws = torch.empty(lib.kronq_workspace_bytes(OP_ATTENTION, heads, dim, n),
+                             dtype=torch.uint8, device=dev)
+        rc = lib.kronq_cache_attention(
+            q.data_ptr(), ldq, n, heads, kv, dim, codes.data_ptr(), params.data_ptr(), pages, page,
+            table.data_ptr(), ldt, table.shape[1], lengths.data_ptr(), seqs, _ptr(starts),
+            int(most), dim ** -0.5 if scale is None else float(scale), int(rotate), out.data_ptr(),
+            ldo, ws.data_ptr(), ws.numel() * ws.element_size(), _stream(dev))
+    _check(rc, "kronq_cache_attention")
+    return out
 
 
 def kronq_layer_loss(W: torch.Tensor, W_hat: Optional[torch.Tensor], HX: torch.Tensor,
