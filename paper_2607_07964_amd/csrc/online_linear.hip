@@ -19,6 +19,7 @@
 // 2^-8, and summed in fp32. For fp32 outputs x' is held in two fp16 planes (value and rest: 22 bits,
 // and never coarser than 2^-32 of the row's largest value) and the weights are exact.
 #include <cmath>
+#include <type_traits>
 
 #include "kq_common.hpp"
 #include "kq_fwht.hpp"
@@ -30,6 +31,7 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+#define KQ_LDS(p) ((__attribute__((address_space(3))) void*)(p))
 
 __device__ __forceinline__ float bf16_f32(uint32_t h) { return __uint_as_float(h << 16); }
 // rounded to nearest even; NaN stays NaN
@@ -390,11 +392,10 @@ __device__ __forceinline__ f32x16_t mfma(u32x4_t a, u32x4_t b, f32x16_t c) {
                                                 __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
 }
 
-// A workgroup of four waves takes 128 RT rows of W (32 RT a wave) and a tile of NT units of rows of
-// x'; a lane holds the codes of one row of W and half of the columns.
-template <int BITS, int NT, int RT, int PLANES, bool SCALED>
+// Few rows. A workgroup of four waves takes 128 rows of W (32 a wave) and a tile of NT units of rows
+// of x'; a lane holds the codes of one row of W and half of the columns.
+template <int BITS, int NT, int PLANES>
 __global__ __launch_bounds__(256) void linear_mfma(MmArgs A) {
-  static_assert(!SCALED || PLANES == 1, "fp32 outputs take exact weights");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int split = blockIdx.y;
   const int rb = blockIdx.x % A.row_blocks, ti = blockIdx.x / A.row_blocks;
@@ -406,84 +407,249 @@ __global__ __launch_bounds__(256) void linear_mfma(MmArgs A) {
     t = Tile{0, ti * NT, 0, int(A.n_rows)};
   }
   const int g0 = split * A.per, g1 = g0 + A.per < A.ng ? g0 + A.per : A.ng;
-  const int64_t n0 = int64_t(rb) * (128 * RT) + wave * (32 * RT);
+  const int64_t n = int64_t(rb) * 128 + wave * 32 + (lane & 31);
   const int last = (t.hi - 1) >> 5;  // last unit
-  const int64_t us = int64_t(A.ng) * 8 * 512;  // elements of a unit
   const uint16_t* xa[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
-    xa[i] = A.xf + (t.unit + i < last ? t.unit + i : last) * us + lane * 8;
+    xa[i] = A.xf + (t.unit + i < last ? t.unit + i : last) * int64_t(A.ng) * 4096 + lane * 8;
+  const int64_t wr = int64_t(t.expert) * A.d_out + (n < A.d_out ? n : A.d_out - 1);
+  const uint32_t* wp = A.packed + wr * A.ldp + (lane >> 5) * 2 * BITS;
+  f32x16_t acc[NT] = {};
+  for (int g = g0; g < g1; ++g) {
+    uint32_t w[2 * BITS];
+    load_codes<BITS>(w, wp + int64_t(g) * 4 * BITS);
+    const int64_t at = wr * A.ldsz + unsigned(g) / unsigned(A.gpq);
+    const _Float16 nz = _Float16(-1024.f - A.zeros[at]);
+    const float sc = A.scales[at];
+    f32x16_t sum[NT] = {};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const u32x4_t b = spread_int<BITS>(w + (j >> 2) * BITS, j & 3, u2(f16x2_t{nz, nz}));
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const uint16_t* p = xa[i] + (int64_t(g) * 8 + j) * 512;
+        const u32x4_t a = *reinterpret_cast<const u32x4_t*>(p);
+        if constexpr (PLANES == 2)
+          sum[i] = mfma(*reinterpret_cast<const u32x4_t*>(p + A.plane), b, sum[i]);
+        sum[i] = mfma(a, b, sum[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][r] = fmaf(sc, sum[i][r], acc[i][r]);
+  }
+  float* part = A.part + int64_t(split) * A.n_rows * A.d_out;
+  if (n >= A.d_out) return;
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int64_t m0 = int64_t(t.unit + i) * 32 + 4 * (lane >> 5);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int64_t m = m0 + 8 * (r >> 2) + (r & 3);
+      if (m >= t.lo && m < t.hi) part[m * A.d_out + n] = acc[i][r];
+    }
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vm() {  // s_waitcnt vmcnt(N), the other counters free
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+
+// this lane's codes of half a group: one chunk of 32
+template <int BITS>
+struct Chunk {
+  uint32_t w[BITS];
+};
+template <int BITS>
+__device__ __forceinline__ Chunk<BITS> load_chunk(const uint32_t* p) {
+  Chunk<BITS> c;
+  if constexpr (BITS == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    c.w[0] = v.x, c.w[1] = v.y;
+  } else if constexpr (BITS == 3) {
+    c.w[0] = p[0], c.w[1] = p[1], c.w[2] = p[2];
+  } else {
+#pragma unroll
+    for (int k = 0; k < BITS; k += 4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p + k);
+      c.w[k] = v.x, c.w[k + 1] = v.y, c.w[k + 2] = v.z, c.w[k + 3] = v.w;
+    }
+  }
+  return c;
+}
+
+// Many rows. As above with x' through LDS: a stage is 64 columns (half a group, a chunk of each
+// lane's codes) of NT units in PLANES planes, NT PLANES = 4 pieces of 4 KB of which each wave brings
+// one by global_load_lds, in fragment order as it stands, through a ring of four stages. One barrier
+// a stage: it publishes the stage and frees the buffer of the one before, which the loads of three
+// stages on then fill. Two workgroups per CU (64 KB of LDS and 256 registers a lane each), so that
+// one wave's spreading of codes runs beside the other's matrix instructions.
+template <int BITS, int NT, int PLANES>
+__global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
+  constexpr int RT = 2, STAGE = 4 * 1024, R = 4;  // (dwords)
+  constexpr bool SCALED = PLANES == 1;
+  static_assert(NT * PLANES == 4, "one piece of a stage per wave");
+  __shared__ __attribute__((aligned(16))) uint32_t lds[R * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // An XCD (workgroup % 8) takes every eighth pair of a row tile and a split, all blocks of W one
+  // after another: the x' of a tile is read through one L2, where its workgroups share it.
+  const int item = int(blockIdx.x & 7) + 8 * int((blockIdx.x >> 3) / A.row_blocks);
+  const int rb = int((blockIdx.x >> 3) % A.row_blocks);
+  const int ti = item / A.splits, split = item % A.splits;
+  Tile t;
+  if (A.tiles) {
+    if (ti >= A.tiles[0].expert) return;
+    t = A.tiles[1 + ti];
+  } else {
+    t = Tile{0, ti * NT, 0, int(A.n_rows)};
+    if (t.unit * 32 >= t.hi) return;
+  }
+  const int g0 = split * A.per, g1 = g0 + A.per < A.ng ? g0 + A.per : A.ng;
+  const int64_t n0 = int64_t(rb) * (128 * RT) + wave * (32 * RT);
+  const int last = (t.hi - 1) >> 5;  // last unit
+  const int nst = 2 * (g1 - g0);
+  const int un = t.unit + wave / PLANES;
+  const uint16_t* src = A.xf + (PLANES == 2 ? (wave & 1) * A.plane : 0) +
+                        ((un < last ? un : last) * int64_t(A.ng) * 8 + int64_t(g0) * 8) * 512 +
+                        lane * 8;
+  auto issue = [&](int st) {  // past the end: the last stage again, never read
+    const uint16_t* p = src + int64_t(st < nst ? st : nst - 1) * 2048;
+    uint32_t* dst = lds + (st & (R - 1)) * STAGE + wave * 1024;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      __builtin_amdgcn_global_load_lds(p + q * 512, KQ_LDS(dst + q * 256), 16, 0, 0);
+  };
   const uint32_t* wp[RT];
   int64_t wr[RT];
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
     const int64_t n = n0 + 32 * i + (lane & 31);
     wr[i] = int64_t(t.expert) * A.d_out + (n < A.d_out ? n : A.d_out - 1);
-    wp[i] = A.packed + wr[i] * A.ldp + (lane >> 5) * 2 * BITS;
+    wp[i] = A.packed + wr[i] * A.ldp + (int64_t(g0) * 4 + (lane >> 5) * 2) * BITS;
   }
-  f32x16_t acc[NT][RT] = {};
-  for (int g = g0; g < g1; ++g) {
-    uint32_t w[RT][2 * BITS], sz[RT];
-    float sc[RT];
+  Chunk<BITS> cw[2][RT];
+  uint32_t sz1[RT];  // of the next group
+  float sc[RT], sc1[RT];
+  auto codes = [&](int st, int h) {  // h = st & 1
+    st = st < nst ? st : nst - 1;
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+      cw[h][i] = load_chunk<BITS>(wp[i] + int64_t(st >> 1) * 4 * BITS + (st & 1) * BITS);
+  };
+  auto params = [&](int gi) {  // of the group gi of this range
+    const int g = g0 + gi < g1 ? g0 + gi : g1 - 1;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-      load_codes<BITS>(w[i], wp[i] + int64_t(g) * 4 * BITS);
       if constexpr (SCALED) {
-        sz[i] = A.table[int64_t(g) * A.w_rows + wr[i]];
+        sz1[i] = A.table[int64_t(g) * A.w_rows + wr[i]];
       } else {
         const int64_t at = wr[i] * A.ldsz + unsigned(g) / unsigned(A.gpq);
-        const _Float16 nz = _Float16(-1024.f - A.zeros[at]);
-        sc[i] = A.scales[at], sz[i] = u2(f16x2_t{nz, nz});
+        sc1[i] = A.scales[at];
+        sz1[i] = __float_as_uint(A.zeros[at]);
       }
     }
-    f32x16_t sum[SCALED ? 1 : NT][SCALED ? 1 : RT] = {};
+  };
+  f32x16_t acc[NT][RT] = {}, sum[SCALED ? 1 : NT][SCALED ? 1 : RT] = {};
+  params(0);
+  codes(0, 0);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      u32x4_t b[RT];
+  for (int st = 0; st < 3; ++st) issue(st);
+  uint32_t z[RT];
+  auto stage = [&](int st, auto hc) {
+    constexpr int h = decltype(hc)::value;
+    // this stage's loads have landed: those of the two stages after it may be out, and what this
+    // wave has requested of codes since
+    wait_vm<8>();
+    __builtin_amdgcn_s_barrier();
+    codes(st + 1, h ^ 1);
+    if constexpr (h == 0) {
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
-        b[i] = SCALED ? spread<BITS>(w[i] + (j >> 2) * BITS, j & 3, sz[i])
-                      : spread_int<BITS>(w[i] + (j >> 2) * BITS, j & 3, sz[i]);
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        const uint16_t* p = xa[i] + (int64_t(g) * 8 + j) * 512;
-        const u32x4_t a = *reinterpret_cast<const u32x4_t*>(p);
-        u32x4_t al = a;
-        if constexpr (PLANES == 2) al = *reinterpret_cast<const u32x4_t*>(p + A.plane);
-#pragma unroll
-        for (int k = 0; k < RT; ++k) {
-          if constexpr (SCALED) {
-            acc[i][k] = mfma(a, b[k], acc[i][k]);
-          } else {
-            if constexpr (PLANES == 2) sum[i][k] = mfma(al, b[k], sum[i][k]);
-            sum[i][k] = mfma(a, b[k], sum[i][k]);
-          }
+      for (int i = 0; i < RT; ++i) {
+        z[i] = sz1[i], sc[i] = sc1[i];
+        if constexpr (!SCALED) {
+          const _Float16 nz = _Float16(-1024.f - __uint_as_float(sz1[i]));
+          z[i] = u2(f16x2_t{nz, nz});
         }
       }
+      params((st >> 1) + 1);
     }
-    if constexpr (!SCALED) {
+    issue(st + 3);
+    const uint32_t* buf = lds + (st & (R - 1)) * STAGE + lane * 4;
+    u32x4_t a[2][4];
+    auto frags = [&](int q) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        a[q & 1][i] = *reinterpret_cast<const u32x4_t*>(buf + i * 1024 + q * 256);
+    };
+    frags(0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (q < 3) frags(q + 1);
+      u32x4_t b[RT];
+#pragma unroll
+      for (int k = 0; k < RT; ++k)
+        b[k] = SCALED ? spread<BITS>(cw[h][k].w, q, z[k]) : spread_int<BITS>(cw[h][k].w, q, z[k]);
 #pragma unroll
       for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int k = 0; k < RT; ++k)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][k][r] = fmaf(sc[k], sum[i][k][r], acc[i][k][r]);
+        for (int k = 0; k < RT; ++k) {
+          if constexpr (SCALED) {
+            acc[i][k] = mfma(a[q & 1][i], b[k], acc[i][k]);
+          } else {
+            sum[i][k] = mfma(a[q & 1][2 * i + 1], b[k], sum[i][k]);
+            sum[i][k] = mfma(a[q & 1][2 * i], b[k], sum[i][k]);
+          }
+        }
+      __builtin_amdgcn_sched_barrier(0);  // (else every step's operands are read at once, and spill)
     }
+    if constexpr (!SCALED) {
+      if constexpr (h == 1) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int k = 0; k < RT; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              acc[i][k][r] = fmaf(sc[k], sum[i][k][r], acc[i][k][r]);
+              sum[i][k][r] = 0.f;
+            }
+      }
+    }
+  };
+  for (int st = 0; st < nst; st += 2) {
+    stage(st, std::integral_constant<int, 0>{});
+    stage(st + 1, std::integral_constant<int, 1>{});
   }
+  wait_vm<0>();  // (loads past the end still write to LDS)
   float* part = A.part + int64_t(split) * A.n_rows * A.d_out;
 #pragma unroll
   for (int k = 0; k < RT; ++k) {
     const int64_t n = n0 + 32 * k + (lane & 31);
     const float unit = SCALED ? A.w_unit[wr[k]] : 1.f;
-    if (n >= A.d_out) continue;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const int64_t m0 = int64_t(t.unit + i) * 32 + 4 * (lane >> 5);
+      const int mu = (t.unit + i) * 32, m0 = mu + 4 * (lane >> 5);
+      float* p = part + int64_t(m0) * A.d_out + n;
+      if (mu >= t.lo && mu + 32 <= t.hi) {  // (uniform) every row of the unit is the tile's
+        if (n < A.d_out) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int64_t m = m0 + 8 * (r >> 2) + (r & 3);
-        if (m >= t.lo && m < t.hi) part[m * A.d_out + n] = acc[i][k][r] * unit;
+          for (int r = 0; r < 16; ++r) {
+            *p = acc[i][k][r] * unit;
+            p += (r & 3) == 3 ? 5 * A.d_out : A.d_out;
+          }
+        }
+      } else if (n < A.d_out) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int m = m0 + 8 * (r >> 2) + (r & 3);
+          if (m >= t.lo && m < t.hi) *p = acc[i][k][r] * unit;
+          p += (r & 3) == 3 ? 5 * A.d_out : A.d_out;
+        }
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 }
@@ -584,21 +750,21 @@ __global__ __launch_bounds__(256) void linear_out(OutArgs A) {
 constexpr int64_t GEMV_ROWS = 4, GEMV_INPUTS = 32768;
 
 struct Plan {
-  int planes, nt, rt, splits, per, rows_in;
-  bool scaled;
+  int planes, nt, splits, per, rows_in;
+  bool ring, scaled;
   int64_t tiles, row_blocks;
 };
 
 Plan make_plan(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts, int y_dtype) {
   Plan p;
   p.planes = y_dtype == KRONQ_BF16 ? 1 : 2;
-  const int64_t per_expert = cdiv(n_rows, n_experts);
-  p.scaled = p.planes == 1 && per_expert > 64;
-  p.nt = p.scaled ? 4 : per_expert > 32 ? 2 : 1;
-  p.rt = p.scaled ? 2 : 1;
+  const int64_t per_expert = cdiv(n_rows, n_experts), ng = d_in / 128;
+  p.ring = per_expert > 64;
+  p.scaled = p.ring && p.planes == 1;
+  p.nt = p.ring ? 4 / p.planes : per_expert > 32 ? 2 : 1;
   p.tiles = n_experts == 1 ? cdiv(n_rows, 32 * p.nt) : most_tiles(n_rows, n_experts, p.nt);
-  p.row_blocks = cdiv(d_out, 128 * p.rt);
-  const int64_t ng = d_in / 128, wgs = p.tiles * p.row_blocks;
+  p.row_blocks = cdiv(d_out, p.ring ? 256 : 128);
+  const int64_t wgs = p.tiles * p.row_blocks;
   int64_t s = wgs < 512 ? 512 / wgs : 1;
   if (s > ng) s = ng;
   if (s > 16) s = 16;
@@ -641,12 +807,17 @@ int launch_in(const InArgs& a, int64_t blocks, int rows_in, hipStream_t s) {
 
 template <int BITS>
 int launch_mm(const MmArgs& a, const Plan& p, hipStream_t s) {
+  if (p.ring) {
+    const dim3 grid(static_cast<unsigned>(8 * cdiv(p.tiles * p.splits, 8) * p.row_blocks));
+    return p.planes == 1
+               ? launch("linear_ring", linear_ring<BITS, 4, 1>, grid, dim3(256), 0, s, a)
+               : launch("linear_ring", linear_ring<BITS, 2, 2>, grid, dim3(256), 0, s, a);
+  }
   const dim3 grid(static_cast<unsigned>(p.tiles * p.row_blocks), static_cast<unsigned>(p.splits));
-#define KQ_MM(NT_, RT_, PL_, SC_)                                                            \
-  launch("linear_mfma", linear_mfma<BITS, NT_, RT_, PL_, SC_>, grid, dim3(256), 0, s, a)
-  if (p.scaled) return KQ_MM(4, 2, 1, true);
-  if (p.planes == 1) return p.nt == 1 ? KQ_MM(1, 1, 1, false) : KQ_MM(2, 1, 1, false);
-  return p.nt == 1 ? KQ_MM(1, 1, 2, false) : KQ_MM(2, 1, 2, false);
+#define KQ_MM(NT_, PL_) \
+  launch("linear_mfma", linear_mfma<BITS, NT_, PL_>, grid, dim3(256), 0, s, a)
+  if (p.planes == 1) return p.nt == 1 ? KQ_MM(1, 1) : KQ_MM(2, 1);
+  return p.nt == 1 ? KQ_MM(1, 2) : KQ_MM(2, 2);
 #undef KQ_MM
 }
 
