@@ -512,15 +512,19 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
   const int last = (t.hi - 1) >> 5;  // last unit
   const int nst = 2 * (g1 - g0);
   const int un = t.unit + wave / PLANES;
-  const uint16_t* src = A.xf + (PLANES == 2 ? (wave & 1) * A.plane : 0) +
-                        ((un < last ? un : last) * int64_t(A.ng) * 8 + int64_t(g0) * 8) * 512 +
-                        lane * 8;
+  // (buffer loads: beside global_load_lds the compiler waits for every outstanding load before it
+  // uses one that went to a register)
+  const uint16_t* const piece = A.xf + (PLANES == 2 ? (wave & 1) * A.plane : 0) +
+                                (un < last ? un : last) * int64_t(A.ng) * 4096;
+  const auto src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(piece), 0, A.ng * 8192,
+                                                     0x00027000);
   auto issue = [&](int st) {  // past the end: the last stage again, never read
-    const uint16_t* p = src + int64_t(st < nst ? st : nst - 1) * 2048;
+    const int at = (2 * g0 + (st < nst ? st : nst - 1)) * 4096;
     uint32_t* dst = lds + (st & (R - 1)) * STAGE + wave * 1024;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-      __builtin_amdgcn_global_load_lds(p + q * 512, KQ_LDS(dst + q * 256), 16, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, KQ_LDS(dst + q * 256), 16, lane * 16,
+                                               at + q * 1024, 0, 0);
   };
   const uint32_t* wp[RT];
   int64_t wr[RT];
@@ -555,6 +559,7 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
   f32x16_t acc[NT][RT] = {}, sum[SCALED ? 1 : NT][SCALED ? 1 : RT] = {};
   params(0);
   codes(0, 0);
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int st = 0; st < 3; ++st) issue(st);
   uint32_t z[RT];
@@ -576,7 +581,10 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
       }
       params((st >> 1) + 1);
     }
+    // (the codes before the rows: their wait then leaves the rows of later stages in flight)
+    __builtin_amdgcn_sched_barrier(0);
     issue(st + 3);
+    __builtin_amdgcn_sched_barrier(0);
     const uint32_t* buf = lds + (st & (R - 1)) * STAGE + lane * 4;
     u32x4_t a[2][4];
     auto frags = [&](int q) {
