@@ -483,9 +483,9 @@ __device__ __forceinline__ Chunk<BITS> load_chunk(const uint32_t* p) {
 
 // Many rows. As above with x' through LDS: a stage is 64 columns (half a group, a chunk of each
 // lane's codes) of NT units in PLANES planes, NT PLANES = 4 pieces of 4 KB of which each wave brings
-// one by global_load_lds, in fragment order as it stands, through a ring of four stages. One barrier
-// a stage: it publishes the stage and frees the buffer of the one before, which the loads of three
-// stages on then fill. Two workgroups per CU (64 KB of LDS and 256 registers a lane each), so that
+// one straight to LDS, in fragment order as it stands, through a ring of four stages. One barrier a
+// stage, in its middle: it publishes the next stage and frees the buffer of the one before, which the
+// loads of three stages on then fill; operands are read one step of 16 columns ahead. Two workgroups per CU (64 KB of LDS and 256 registers a lane each), so that
 // one wave's spreading of codes runs beside the other's matrix instructions.
 template <int BITS, int NT, int PLANES>
 __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
@@ -562,13 +562,15 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int st = 0; st < 3; ++st) issue(st);
+  u32x4_t a[2][4];
+  auto frags = [&](int st, int q) {
+    const uint32_t* buf = lds + (st & (R - 1)) * STAGE + lane * 4 + q * 256;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[q & 1][i] = *reinterpret_cast<const u32x4_t*>(buf + i * 1024);
+  };
   uint32_t z[RT];
   auto stage = [&](int st, auto hc) {
     constexpr int h = decltype(hc)::value;
-    // this stage's loads have landed: those of the two stages after it may be out, and what this
-    // wave has requested of codes since
-    wait_vm<8>();
-    __builtin_amdgcn_s_barrier();
     codes(st + 1, h ^ 1);
     if constexpr (h == 0) {
 #pragma unroll
@@ -581,21 +583,18 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
       }
       params((st >> 1) + 1);
     }
-    // (the codes before the rows: their wait then leaves the rows of later stages in flight)
     __builtin_amdgcn_sched_barrier(0);
-    issue(st + 3);
-    __builtin_amdgcn_sched_barrier(0);
-    const uint32_t* buf = lds + (st & (R - 1)) * STAGE + lane * 4;
-    u32x4_t a[2][4];
-    auto frags = [&](int q) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        a[q & 1][i] = *reinterpret_cast<const u32x4_t*>(buf + i * 1024 + q * 256);
-    };
-    frags(0);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      if (q < 3) frags(q + 1);
+      if (q == 2) {
+        // the next stage's loads have landed (those of the one after it may be out, and what this
+        // wave has requested of codes since)
+        wait_vm<8>();
+        __builtin_amdgcn_s_barrier();
+        issue(st + 3);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      frags(q < 3 ? st : st + 1, (q + 1) & 3);
       u32x4_t b[RT];
 #pragma unroll
       for (int k = 0; k < RT; ++k)
@@ -627,6 +626,9 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
       }
     }
   };
+  wait_vm<8>();
+  __builtin_amdgcn_s_barrier();
+  frags(0, 0);
   for (int st = 0; st < nst; st += 2) {
     stage(st, std::integral_constant<int, 0>{});
     stage(st + 1, std::integral_constant<int, 1>{});
