@@ -21,8 +21,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "kq_common.hpp"
-#include "kq_fwht.hpp"
+#include "kq_linear.hpp"
 
 namespace kq {
 namespace {
@@ -33,28 +32,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 #define KQ_LDS(p) ((__attribute__((address_space(3))) void*)(p))
 
-__device__ __forceinline__ float bf16_f32(uint32_t h) { return __uint_as_float(h << 16); }
-// rounded to nearest even; NaN stays NaN
-__device__ __forceinline__ uint16_t f32_bf16(float v) {
-  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
-}
-__device__ __forceinline__ float pow2f(int e) { return __uint_as_float(uint32_t(127 + e) << 23); }
-
-// Column (of a chunk of 32) of element i of step jj of a lane's eight codes, in the order in which
-// the codes of a packed chunk are spread to pairs of fp16 (spread below).
-__device__ __forceinline__ int chunk_col(int bits, int jj, int i) {
-  const int p = i >> 1, b = i & 1;
-  if (bits == 2) return 16 * (jj >> 1) + 4 * (jj & 1) + p + 8 * b;
-  if (bits == 8) return 8 * jj + 4 * (p >> 1) + (p & 1) + 2 * b;
-  return 8 * jj + p + 4 * b;  // 3 and 4 bits
-}
-
-// ---- row tiles ---------------------------------------------------------------------------------
-// Rows are taken in units of 32 (row / 32); a tile is up to NT units of one expert, and the rows of
-// a unit outside [lo, hi) belong to another tile. One layer without offsets has one expert.
-struct Tile {
-  int expert, unit, lo, hi;
-};
+using Tile = LinearTile;
 
 // tiles that any offsets of n_experts over n_rows rows can give: the experts' ranges overlap at
 // most n_rows / 32 + 1 units once and one more for each expert after the first, and each expert's
@@ -62,221 +40,6 @@ struct Tile {
 __host__ __device__ inline int64_t most_tiles(int64_t n_rows, int64_t n_experts, int nt) {
   const int64_t e = n_experts < n_rows ? n_experts : n_rows;
   return (cdiv(n_rows, 32) + e - 1) / nt + e;
-}
-
-// ---- 1. input side -----------------------------------------------------------------------------
-struct InArgs {
-  const void* x;
-  int64_t ldx;
-  int64_t n_rows, d_in;
-  const float* mul;
-  const float* q28;
-  int m, rotate, has28, bits, planes;
-  float norm;
-  uint16_t* xf;       // fragment order, plane after plane
-  int64_t plane;      // elements of a plane
-  float* row_unit;    // [n_rows] what the rows were divided by
-  // weights' table: per group and row a dword {s 2^24 / unit, -z s / unit} in fp16; per row its unit
-  const float *scales, *zeros;
-  int64_t ldsz;
-  int gpq, ng;        // groups of 128 columns per quantisation group, and in a row
-  int64_t w_rows;     // rows of W over all experts
-  uint32_t* table;
-  float* w_unit;
-  // experts
-  const int* offsets;
-  int n_experts, nt;
-  int64_t max_tiles;
-  Tile* tiles;        // max_tiles of them after a count (in its own slot of 16 bytes)
-  int64_t table_blocks;
-};
-
-__device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
-
-// The list of tiles, by one workgroup of 256 threads: the experts' ranges made ascending and cut to
-// [0, n_rows), so that no content of offsets leads out of the rows.
-__device__ void list_tiles(const InArgs& A, int* sh) {
-  const int tid = threadIdx.x, n = int(A.n_rows);
-  int base = 0, top = clampi(A.offsets[0], 0, n);  // tiles so far, largest offset so far
-  for (int e0 = 0; e0 < A.n_experts; e0 += 256) {
-    const int e = e0 + tid;
-    int v = e < A.n_experts ? clampi(A.offsets[e + 1], 0, n) : 0;
-    for (int o = 1; o < 256; o <<= 1) {  // running maximum over the threads
-      sh[tid] = v;
-      __syncthreads();
-      if (tid >= o) v = max(v, sh[tid - o]);
-      __syncthreads();
-    }
-    v = max(v, top);
-    sh[tid] = v;
-    __syncthreads();
-    const int lo = tid ? sh[tid - 1] : top, hi = v;
-    top = sh[255];
-    __syncthreads();
-    const int u0 = lo >> 5, nu = hi > lo ? ((hi - 1) >> 5) - u0 + 1 : 0;
-    const int k = (nu + A.nt - 1) / A.nt;
-    int sum = k;
-    for (int o = 1; o < 256; o <<= 1) {
-      sh[tid] = sum;
-      __syncthreads();
-      if (tid >= o) sum += sh[tid - o];
-      __syncthreads();
-    }
-    for (int i = 0; i < k; ++i) {
-      const int64_t at = base + sum - k + i;
-      if (at < A.max_tiles) A.tiles[1 + at] = Tile{e, u0 + i * A.nt, lo, hi};
-    }
-    sh[tid] = sum;
-    __syncthreads();
-    base += sh[255];
-    __syncthreads();
-  }
-  if (tid == 0) A.tiles[0] = Tile{base < A.max_tiles ? base : int(A.max_tiles), 0, 0, 0};
-}
-
-// the table of eight rows of W: 32 threads take a row
-__device__ void fill_table(const InArgs& A, int64_t block) {
-  const int64_t row = block * 8 + (threadIdx.x >> 5);
-  const int t = threadIdx.x & 31;
-  if (row >= A.w_rows) return;
-  const float *s = A.scales + row * A.ldsz, *z = A.zeros + row * A.ldsz;
-  const int nq = A.ng / A.gpq;
-  float mx = 0.f;
-  for (int g = t; g < nq; g += 32) mx = fmaxf(mx, fabsf(s[g]));
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-  // s 2^24 / unit in [2^14, 2^15): unit = 2^(e + 10) for a largest scale in [2^e, 2^(e + 1))
-  const int e = int(__float_as_uint(mx) >> 23) - 127;
-  const int ue = mx > 0.f && e < 128 ? clampi(e + 10, -100, 120) : 0;
-  const float up = pow2f(-ue);
-  for (int g = t; g < A.ng; g += 32) {
-    const float sn = s[g / A.gpq] * up;
-    const f16x2_t o = {_Float16(sn * 16777216.f), _Float16(-z[g / A.gpq] * sn)};
-    A.table[int64_t(g) * A.w_rows + row] = __builtin_bit_cast(uint32_t, o);
-  }
-  if (t == 0) A.w_unit[row] = pow2f(ue);
-}
-
-// out[a] = sum_k Q[a][k] in[k] over the 28 segments of each of R rows in LDS (Q in LDS, transposed
-// when q_trans): a thread takes one column
-__device__ __forceinline__ void mix28(float* buf, int R, int m, const float* Q, int tid, int nthr) {
-  for (int c = tid; c < R * m; c += nthr) {
-    float* col = buf + (c / m) * 28 * m + (c % m);
-    float v[28];
-#pragma unroll
-    for (int k = 0; k < 28; ++k) v[k] = col[k * m];
-#pragma unroll 4
-    for (int a = 0; a < 28; ++a) {
-      float s = 0.f;
-#pragma unroll
-      for (int k = 0; k < 28; ++k) s = fmaf(Q[a * 28 + k], v[k], s);
-      col[a * m] = s;
-    }
-  }
-}
-
-// A workgroup of 256 threads takes R rows through LDS (R rows of a unit side by side, so that its
-// 16-byte pieces in fragment order are 16 R bytes together).
-template <typename T, int R>
-__global__ __launch_bounds__(256) void linear_in(InArgs A) {
-  extern __shared__ __attribute__((aligned(16))) float buf[];  // R rows of d_in floats
-  __shared__ float Q[28 * 28];
-  __shared__ float red[4 * R];
-  __shared__ int sh[256];
-  const int tid = threadIdx.x;
-  int64_t block = blockIdx.x;
-  if (block < A.table_blocks) return fill_table(A, block);
-  block -= A.table_blocks;
-  if (A.offsets) {
-    if (block == 0) return list_tiles(A, sh);
-    --block;
-  }
-  const int64_t r0 = block * R;
-  const int d = int(A.d_in);
-  const int rows = A.n_rows - r0 < R ? int(A.n_rows - r0) : R;
-  for (int r = 0; r < rows; ++r) {
-    int64_t expert = 0;
-    if (A.offsets) {  // experts whose range ends at or before this row
-      int n = 0;
-      for (int e0 = 0; e0 < A.n_experts; e0 += 256) {
-        const int e = e0 + tid;
-        n += __syncthreads_count(e < A.n_experts && A.offsets[e + 1] <= r0 + r);
-      }
-      if (n >= A.n_experts || r0 + r < A.offsets[0]) continue;  // (uniform) a row of none
-      expert = n;
-    }
-    if (A.has28 && (r == 0 || A.offsets)) {
-      const float* q = A.q28 + expert * 784;
-      for (int i = tid; i < 784; i += 256) Q[i] = q[i];
-    }
-    const T* x = static_cast<const T*>(A.x) + (r0 + r) * A.ldx;
-    const float* mul = A.mul ? A.mul + expert * d : nullptr;
-    float* b = buf + r * d;
-    for (int j = 8 * tid; j < d; j += 8 * 256) {
-      float v[8];
-      if constexpr (sizeof(T) == 2) {
-        const uint4 w = *reinterpret_cast<const uint4*>(x + j);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          v[2 * k] = bf16_f32(u[k] & 0xFFFFu);
-          v[2 * k + 1] = __uint_as_float(u[k] & 0xFFFF0000u);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; k += 4) {
-          const float4 w = *reinterpret_cast<const float4*>(x + j + k);
-          v[k] = w.x, v[k + 1] = w.y, v[k + 2] = w.z, v[k + 3] = w.w;
-        }
-      }
-      if (mul) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= mul[j + k];
-      }
-#pragma unroll
-      for (int k = 0; k < 8; k += 4)
-        *reinterpret_cast<float4*>(b + j + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
-    }
-    __syncthreads();
-    if (A.rotate) {
-      fwht_lds(b, d, A.m, tid, 256);
-      if (A.has28) {
-        mix28(b, 1, A.m, Q, tid, 256);
-        __syncthreads();
-      }
-    }
-    float mx = 0.f;
-    for (int j = tid; j < d; j += 256) mx = fmaxf(mx, fabsf(b[j]));
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-    if ((tid & 63) == 0) red[4 * r + (tid >> 6)] = mx;
-    __syncthreads();
-  }
-  // one thread per 8 columns of a row, the rows side by side
-  const int64_t unit = r0 >> 5;
-  for (int i = tid; i < R * (d / 8); i += 256) {
-    const int r = i % R, piece = i / R;  // piece = 2 ks + h, ks the step of 16 columns
-    if (r >= rows) continue;
-    const float mx = fmaxf(fmaxf(red[4 * r], red[4 * r + 1]), fmaxf(red[4 * r + 2], red[4 * r + 3])) *
-                     A.norm;
-    const int e = int(__float_as_uint(mx) >> 23) - 127;
-    const int ue = mx > 0.f && e < 128 ? clampi(e - 7, -100, 100) : 0;
-    const float up = pow2f(-ue) * A.norm;
-    if (piece == 0) A.row_unit[r0 + r] = pow2f(ue);
-    const int ks = piece >> 1, h = piece & 1, j = ks & 7;
-    const float* b = buf + r * d + (ks >> 3) * 128 + 64 * h + 32 * (j >> 2);
-    f16x8_t hi, lo;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      float v = b[chunk_col(A.bits, j & 3, k)] * up;
-      asm("" : "+v"(v));  // both planes from the one rounded product (a multiplication merged into
-      hi[k] = _Float16(v);  // one conversion only would round the planes' sum twice)
-      lo[k] = _Float16(v - float(hi[k]));
-    }
-    uint16_t* o = A.xf + ((unit * (d / 16) + ks) * 64 + ((r0 + r) & 31) + 32 * h) * 8;
-    *reinterpret_cast<f16x8_t*>(o) = hi;
-    if (A.planes == 2) *reinterpret_cast<f16x8_t*>(o + A.plane) = lo;
-  }
 }
 
 // ---- 2. products ---------------------------------------------------------------------------------
@@ -294,7 +57,8 @@ struct MmArgs {
   const Tile* tiles;  // null: one layer, unit tiles in order
   int64_t n_rows;
   int row_blocks, splits, per;  // groups per split
-  float* part;        // [split][row][d_out]
+  float* part;        // [split][row][ld]
+  int64_t ld;
 };
 
 __device__ __forceinline__ f16x2_t h2(uint32_t v) { return __builtin_bit_cast(f16x2_t, v); }
@@ -440,7 +204,7 @@ __global__ __launch_bounds__(256) void linear_mfma(MmArgs A) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][r] = fmaf(sc, sum[i][r], acc[i][r]);
   }
-  float* part = A.part + int64_t(split) * A.n_rows * A.d_out;
+  float* part = A.part + int64_t(split) * A.n_rows * A.ld;
   if (n >= A.d_out) return;
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
@@ -448,7 +212,7 @@ __global__ __launch_bounds__(256) void linear_mfma(MmArgs A) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int64_t m = m0 + 8 * (r >> 2) + (r & 3);
-      if (m >= t.lo && m < t.hi) part[m * A.d_out + n] = acc[i][r];
+      if (m >= t.lo && m < t.hi) part[m * A.ld + n] = acc[i][r];
     }
   }
 }
@@ -634,7 +398,7 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
     stage(st + 1, std::integral_constant<int, 1>{});
   }
   wait_vm<0>();  // (loads past the end still write to LDS)
-  float* part = A.part + int64_t(split) * A.n_rows * A.d_out;
+  float* part = A.part + int64_t(split) * A.n_rows * A.ld;
 #pragma unroll
   for (int k = 0; k < RT; ++k) {
     const int64_t n = n0 + 32 * k + (lane & 31);
@@ -642,13 +406,13 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const int mu = (t.unit + i) * 32, m0 = mu + 4 * (lane >> 5);
-      float* p = part + int64_t(m0) * A.d_out + n;
+      float* p = part + int64_t(m0) * A.ld + n;
       if (mu >= t.lo && mu + 32 <= t.hi) {  // (uniform) every row of the unit is the tile's
         if (n < A.d_out) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             *p = acc[i][k][r] * unit;
-            p += (r & 3) == 3 ? 5 * A.d_out : A.d_out;
+            p += (r & 3) == 3 ? 5 * A.ld : A.ld;
           }
         }
       } else if (n < A.d_out) {
@@ -656,102 +420,11 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
         for (int r = 0; r < 16; ++r) {
           const int m = m0 + 8 * (r >> 2) + (r & 3);
           if (m >= t.lo && m < t.hi) *p = acc[i][k][r] * unit;
-          p += (r & 3) == 3 ? 5 * A.d_out : A.d_out;
+          p += (r & 3) == 3 ? 5 * A.ld : A.ld;
         }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-  }
-}
-
-// ---- 3. output side ------------------------------------------------------------------------------
-struct OutArgs {
-  const float* part;     // [split][row][d_out]
-  int64_t stride;        // of a split
-  int splits;
-  const float* row_unit;  // or null (1)
-  int64_t n_rows, d_out;
-  const float* mul;
-  const float* q28;
-  int m, rotate, has28;
-  float norm;
-  const float* bias;
-  int act;
-  const void* residual;
-  int64_t ldr;
-  void* y;
-  int64_t ldy;
-  const int* offsets;
-  int n_experts;
-};
-
-__device__ __forceinline__ float activate(float z, int act) {
-  switch (act) {
-    case KRONQ_ACT_RELU:
-      return z < 0.f ? 0.f : z;  // (NaN stays)
-    case KRONQ_ACT_GELU:
-      return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    case KRONQ_ACT_SILU:
-      return z / (1.f + expf(-z));
-    default:
-      return z;
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ float load1(const void* p, int64_t i) {
-  if constexpr (sizeof(T) == 2) return bf16_f32(static_cast<const uint16_t*>(p)[i]);
-  return static_cast<const float*>(p)[i];
-}
-
-// A workgroup of 256 threads takes a row through LDS.
-template <typename T>
-__global__ __launch_bounds__(256) void linear_out(OutArgs A) {
-  extern __shared__ __attribute__((aligned(16))) float buf[];  // d_out floats
-  __shared__ float Q[28 * 28];
-  const int tid = threadIdx.x, d = int(A.d_out);
-  const int64_t row = blockIdx.x;
-  int64_t expert = 0;
-  if (A.offsets) {
-    int n = 0;
-    for (int e0 = 0; e0 < A.n_experts; e0 += 256) {
-      const int e = e0 + tid;
-      n += __syncthreads_count(e < A.n_experts && A.offsets[e + 1] <= row);
-    }
-    if (n >= A.n_experts || row < A.offsets[0]) return;
-    expert = n;
-  }
-  const float* src = A.part + row * A.d_out;
-  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.norm;
-  for (int j = tid; j < d; j += 256) {
-    float v = src[j];
-    for (int s = 1; s < A.splits; ++s) v += src[s * A.stride + j];
-    buf[j] = v;
-  }
-  if (A.has28) {  // the transposed factor
-    const float* q = A.q28 + expert * 784;
-    for (int i = tid; i < 784; i += 256) Q[(i % 28) * 28 + i / 28] = q[i];
-  }
-  __syncthreads();
-  if (A.rotate) {
-    fwht_lds(buf, d, A.m, tid, 256);
-    if (A.has28) {
-      mix28(buf, 1, A.m, Q, tid, 256);
-      __syncthreads();
-    }
-  }
-  const float* mul = A.mul ? A.mul + expert * d : nullptr;
-  const float* bias = A.bias ? A.bias + expert * d : nullptr;
-  for (int j = tid; j < d; j += 256) {
-    float v = buf[j] * up;
-    if (mul) v *= mul[j];
-    if (bias) v += bias[j];
-    v = activate(v, A.act);
-    if (A.residual) v += load1<T>(A.residual, row * A.ldr + j);
-    if constexpr (sizeof(T) == 2)
-      static_cast<uint16_t*>(A.y)[row * A.ldy + j] = f32_bf16(v);
-    else
-      static_cast<float*>(A.y)[row * A.ldy + j] = v;
   }
 }
 
@@ -760,7 +433,7 @@ __global__ __launch_bounds__(256) void linear_out(OutArgs A) {
 constexpr int64_t GEMV_ROWS = 4, GEMV_INPUTS = 32768;
 
 struct Plan {
-  int planes, nt, splits, per, rows_in;
+  int planes, nt, splits, per;
   bool ring, scaled;
   int64_t tiles, row_blocks;
 };
@@ -780,7 +453,6 @@ Plan make_plan(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts, i
   if (s > 16) s = 16;
   p.per = int(cdiv(ng, s));
   p.splits = int(cdiv(ng, p.per));
-  p.rows_in = d_in <= 4096 && n_rows >= 1024 ? 4 : 1;
   return p;
 }
 
@@ -798,21 +470,13 @@ Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, i
   Ws w;
   w.xf = cv.take<uint16_t>(size_t(p.planes) * size_t(cdiv(n_rows, 32) * 32) * size_t(d_in));
   w.row_unit = cv.take<float>(size_t(n_rows));
-  w.part = cv.take<float>(size_t(p.splits) * size_t(n_rows) * size_t(d_out));
+  w.part = cv.take<float>(size_t(p.splits) * size_t(n_rows) * size_t(cdiv(d_out, 8) * 8));
   const size_t w_rows = p.scaled ? size_t(n_experts) * size_t(d_out) : 0;
   w.w_unit = cv.take<float>(w_rows);
   w.table = cv.take<uint32_t>(w_rows * size_t(d_in / 128));
   w.tiles = cv.take<Tile>(grouped ? size_t(p.tiles) + 1 : 0);
   w.bytes = align256(cv.used) + 256;
   return w;
-}
-
-template <typename T>
-int launch_in(const InArgs& a, int64_t blocks, int rows_in, hipStream_t s) {
-  const size_t lds = size_t(rows_in) * size_t(a.d_in) * sizeof(float);
-  const dim3 grid(static_cast<unsigned>(blocks));
-  if (rows_in == 4) return launch("linear_in", linear_in<T, 4>, grid, dim3(256), lds, s, a);
-  return launch("linear_in", linear_in<T, 1>, grid, dim3(256), lds, s, a);
 }
 
 template <int BITS>
@@ -831,14 +495,6 @@ int launch_mm(const MmArgs& a, const Plan& p, hipStream_t s) {
 #undef KQ_MM
 }
 
-// order and normalisation of a side's transform
-void rot_plan(int64_t d, bool rotate, int& m, int& has28, float& norm) {
-  const RotDim rd = rot_dim(d);
-  has28 = rotate && rd.has28;
-  m = rotate ? int(rd.m) : 1;
-  norm = rotate ? float(1.0 / std::sqrt(double(rd.m))) : 1.f;
-}
-
 }  // namespace
 
 size_t linear_ws_bytes(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts) {
@@ -853,52 +509,47 @@ size_t linear_ws_bytes(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_ex
 }
 
 int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
-  OutArgs o{};
+  LinearOut o{};
   o.n_rows = j.n_rows, o.d_out = j.d_out, o.mul = j.mul_out, o.q28 = j.q28_out;
-  o.rotate = (j.flags & KRONQ_ROT_OUT) != 0;
-  rot_plan(j.d_out, o.rotate, o.m, o.has28, o.norm);
+  o.turn = linear_turn(j.d_out, (j.flags & KRONQ_ROT_OUT) != 0);
   o.bias = j.bias, o.act = j.act, o.residual = j.residual, o.ldr = j.ldr;
-  o.y = j.y, o.ldy = j.ldy, o.offsets = j.offsets, o.n_experts = int(j.n_experts);
+  o.y = j.y, o.y_dtype = j.y_dtype, o.ldy = j.ldy;
+  o.offsets = j.offsets, o.n_experts = int(j.n_experts);
   if (!j.offsets && j.n_rows <= GEMV_ROWS && j.n_rows * j.d_in <= GEMV_INPUTS) {
     float* yr;
     KQ_TRY(online_product_launch(j.packed, j.ldp, j.scales, j.zeros, j.ldsz, j.bits, j.group,
                                  j.d_out, j.d_in, j.mul_in, j.q28_in, j.flags, j.x, j.x_dtype,
                                  j.ldx, j.n_rows, ws, &yr, s));
-    o.part = yr, o.splits = 1;
-  } else {
-    const Plan p = make_plan(j.d_out, j.d_in, j.n_rows, j.n_experts, j.y_dtype);
-    const Ws w = carve(ws, p, j.d_out, j.d_in, j.n_rows, j.n_experts, true);
-    InArgs a{};
-    a.x = j.x, a.ldx = j.ldx, a.n_rows = j.n_rows, a.d_in = j.d_in;
-    a.mul = j.mul_in, a.q28 = j.q28_in, a.rotate = (j.flags & KRONQ_ROT_IN) != 0;
-    rot_plan(j.d_in, a.rotate, a.m, a.has28, a.norm);
-    a.bits = j.bits, a.planes = p.planes, a.xf = w.xf, a.row_unit = w.row_unit;
-    a.plane = cdiv(j.n_rows, 32) * 32 * j.d_in;
-    a.scales = j.scales, a.zeros = j.zeros, a.ldsz = j.ldsz;
-    a.gpq = j.group / 128, a.ng = int(j.d_in / 128);
-    a.w_rows = j.n_experts * j.d_out, a.table = w.table, a.w_unit = w.w_unit;
-    a.offsets = j.offsets, a.n_experts = int(j.n_experts), a.nt = p.nt;
-    a.max_tiles = p.tiles, a.tiles = w.tiles;
-    a.table_blocks = p.scaled ? cdiv(a.w_rows, 8) : 0;
-    const int64_t blocks = a.table_blocks + (j.offsets ? 1 : 0) + cdiv(j.n_rows, p.rows_in);
-    KQ_TRY(j.x_dtype == KRONQ_BF16 ? launch_in<uint16_t>(a, blocks, p.rows_in, s)
-                                   : launch_in<float>(a, blocks, p.rows_in, s));
-    MmArgs m{};
-    m.packed = j.packed, m.ldp = j.ldp, m.d_out = j.d_out, m.w_rows = a.w_rows;
-    m.xf = w.xf, m.plane = a.plane, m.ng = a.ng, m.table = w.table, m.w_unit = w.w_unit;
-    m.scales = j.scales, m.zeros = j.zeros, m.ldsz = j.ldsz, m.gpq = a.gpq;
-    m.tiles = j.offsets ? w.tiles : nullptr, m.n_rows = j.n_rows;
-    m.row_blocks = int(p.row_blocks), m.splits = p.splits, m.per = p.per, m.part = w.part;
-    KQ_TRY(j.bits == 2   ? launch_mm<2>(m, p, s)
-           : j.bits == 3 ? launch_mm<3>(m, p, s)
-           : j.bits == 4 ? launch_mm<4>(m, p, s)
-                         : launch_mm<8>(m, p, s));
-    o.part = w.part, o.stride = j.n_rows * j.d_out, o.splits = p.splits, o.row_unit = w.row_unit;
+    o.part = yr, o.ld = j.d_out, o.splits = 1;
+    return linear_out_launch(o, s);
   }
-  const size_t lds = size_t(j.d_out) * sizeof(float);
-  const dim3 grid(static_cast<unsigned>(j.n_rows));
-  return j.y_dtype == KRONQ_BF16 ? launch("linear_out", linear_out<uint16_t>, grid, dim3(256), lds, s, o)
-                                 : launch("linear_out", linear_out<float>, grid, dim3(256), lds, s, o);
+  const Plan p = make_plan(j.d_out, j.d_in, j.n_rows, j.n_experts, j.y_dtype);
+  const Ws w = carve(ws, p, j.d_out, j.d_in, j.n_rows, j.n_experts, true);
+  LinearIn a{};
+  a.x = j.x, a.x_dtype = j.x_dtype, a.ldx = j.ldx, a.n_rows = j.n_rows, a.d_in = j.d_in;
+  a.mul = j.mul_in, a.q28 = j.q28_in, a.turn = linear_turn(j.d_in, (j.flags & KRONQ_ROT_IN) != 0);
+  a.bits = j.bits, a.planes = p.planes, a.xf = w.xf, a.row_unit = w.row_unit;
+  a.plane = cdiv(j.n_rows, 32) * 32 * j.d_in;
+  a.table = p.scaled ? w.table : nullptr, a.w_unit = w.w_unit;
+  a.scales = j.scales, a.zeros = j.zeros, a.ldsz = j.ldsz;
+  a.gpq = j.group / 128, a.ng = int(j.d_in / 128), a.w_rows = j.n_experts * j.d_out;
+  a.offsets = j.offsets, a.n_experts = int(j.n_experts), a.nt = p.nt;
+  a.max_tiles = p.tiles, a.tiles = w.tiles;
+  KQ_TRY(linear_in_launch(a, s));
+  MmArgs m{};
+  m.packed = j.packed, m.ldp = j.ldp, m.d_out = j.d_out, m.w_rows = a.w_rows;
+  m.xf = w.xf, m.plane = a.plane, m.ng = a.ng, m.table = w.table, m.w_unit = w.w_unit;
+  m.scales = j.scales, m.zeros = j.zeros, m.ldsz = j.ldsz, m.gpq = a.gpq;
+  m.tiles = j.offsets ? w.tiles : nullptr, m.n_rows = j.n_rows;
+  m.row_blocks = int(p.row_blocks), m.splits = p.splits, m.per = p.per;
+  m.part = w.part, m.ld = cdiv(j.d_out, 8) * 8;
+  KQ_TRY(j.bits == 2   ? launch_mm<2>(m, p, s)
+         : j.bits == 3 ? launch_mm<3>(m, p, s)
+         : j.bits == 4 ? launch_mm<4>(m, p, s)
+                       : launch_mm<8>(m, p, s));
+  o.part = w.part, o.ld = m.ld, o.stride = j.n_rows * m.ld, o.splits = p.splits;
+  o.row_unit = w.row_unit;
+  return linear_out_launch(o, s);
 }
 
 }  // namespace kq

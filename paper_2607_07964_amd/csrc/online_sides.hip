@@ -1,0 +1,544 @@
+// Both sides of the served layer (online_linear.hip): the transform of the activations to fp16 in
+// fragment order, and the transform of the products with bias, activation and residual.
+//
+// A transform of order d is A (x) H_m with A = Q28 (or its transpose), or H_d alone. A workgroup of
+// 256 threads takes a row, as d / cols columns of cols = min(m, 512) elements. Its two factors touch
+// the row in two ways that meet once in LDS:
+//   across the columns (A and the upper stages of H): a thread holds the same two elements of every
+//     column, 2 d / cols registers, and mixes them in place;
+//   inside a column (the lower nine stages of H): a lane holds 8 neighbours, three stages in
+//     registers, six across lanes by DPP.
+// The input side goes across first, straight from the row in memory, and ends with 8 neighbours per
+// lane, which is what a 16-byte piece in fragment order takes; the output side goes the other way
+// round, and its epilogue works on neighbours of neighbouring threads. Bound by the reads and writes
+// of the rows; with a 28-point factor by its 28 multiply-adds per element.
+#include <cmath>
+
+#include "kq_fwht.hpp"
+#include "kq_linear.hpp"
+
+namespace kq {
+namespace {
+
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float bf16_f32(uint32_t h) { return __uint_as_float(h << 16); }
+// rounded to nearest even; NaN stays NaN
+__device__ __forceinline__ uint16_t f32_bf16(float v) {
+  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+}
+__device__ __forceinline__ float pow2f(int e) { return __uint_as_float(uint32_t(127 + e) << 23); }
+__device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+// The expert whose rows [offsets[e], offsets[e + 1]) hold this one, or -1. Every thread of the
+// workgroup calls it.
+__device__ __forceinline__ int expert_of(const int* offsets, int n_experts, int64_t row) {
+  int n = 0;  // experts whose range ends at or before the row
+  for (int e0 = 0; e0 < n_experts; e0 += 256) {
+    const int e = e0 + int(threadIdx.x);
+    n += __syncthreads_count(e < n_experts && offsets[e + 1] <= row);
+  }
+  return n >= n_experts || row < offsets[0] ? -1 : n;
+}
+
+// The list of tiles, by one workgroup of 256 threads: the experts' ranges made ascending and cut to
+// [0, n_rows), so that no content of offsets leads out of the rows.
+__device__ void list_tiles(const LinearIn& A, int* sh) {
+  const int tid = threadIdx.x, n = int(A.n_rows);
+  int base = 0, top = clampi(A.offsets[0], 0, n);  // tiles so far, largest offset so far
+  for (int e0 = 0; e0 < A.n_experts; e0 += 256) {
+    const int e = e0 + tid;
+    int v = e < A.n_experts ? clampi(A.offsets[e + 1], 0, n) : 0;
+    for (int o = 1; o < 256; o <<= 1) {  // running maximum over the threads
+      sh[tid] = v;
+      __syncthreads();
+      if (tid >= o) v = max(v, sh[tid - o]);
+      __syncthreads();
+    }
+    v = max(v, top);
+    sh[tid] = v;
+    __syncthreads();
+    const int lo = tid ? sh[tid - 1] : top, hi = v;
+    top = sh[255];
+    __syncthreads();
+    const int u0 = lo >> 5, nu = hi > lo ? ((hi - 1) >> 5) - u0 + 1 : 0;
+    const int k = (nu + A.nt - 1) / A.nt;
+    int sum = k;
+    for (int o = 1; o < 256; o <<= 1) {
+      sh[tid] = sum;
+      __syncthreads();
+      if (tid >= o) sum += sh[tid - o];
+      __syncthreads();
+    }
+    for (int i = 0; i < k; ++i) {
+      const int64_t at = base + sum - k + i;
+      if (at < A.max_tiles) A.tiles[1 + at] = LinearTile{e, u0 + i * A.nt, lo, hi};
+    }
+    sh[tid] = sum;
+    __syncthreads();
+    base += sh[255];
+    __syncthreads();
+  }
+  if (tid == 0) A.tiles[0] = LinearTile{base < A.max_tiles ? base : int(A.max_tiles), 0, 0, 0};
+}
+
+// the table of eight rows of W: 32 threads take a row
+__device__ void fill_table(const LinearIn& A, int64_t block) {
+  const int64_t row = block * 8 + (threadIdx.x >> 5);
+  const int t = threadIdx.x & 31;
+  if (row >= A.w_rows) return;
+  const float *s = A.scales + row * A.ldsz, *z = A.zeros + row * A.ldsz;
+  const int nq = A.ng / A.gpq;
+  float mx = 0.f;
+  for (int g = t; g < nq; g += 32) mx = fmaxf(mx, fabsf(s[g]));
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  // s 2^24 / unit in [2^14, 2^15): unit = 2^(e + 10) for a largest scale in [2^e, 2^(e + 1))
+  const int e = int(__float_as_uint(mx) >> 23) - 127;
+  const int ue = mx > 0.f && e < 128 ? clampi(e + 10, -100, 120) : 0;
+  const float up = pow2f(-ue);
+  for (int g = t; g < A.ng; g += 32) {
+    const float sn = s[g / A.gpq] * up;
+    const f16x2_t o = {_Float16(sn * 16777216.f), _Float16(-z[g / A.gpq] * sn)};
+    A.table[int64_t(g) * A.w_rows + row] = __builtin_bit_cast(uint32_t, o);
+  }
+  if (t == 0) A.w_unit[row] = pow2f(ue);
+}
+
+// Butterfly stages of strides 1, 2, 4 (registers) and 8, 16, ... below cols (lanes) on N octets of
+// neighbours a lane, neighbouring octets in neighbouring lanes. cols is a power of two from 8 on.
+template <int N>
+__device__ __forceinline__ void inside_column(float (&x)[8 * N], int lane, int cols) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = x[8 * n + k];
+    hadamard_reg<8>(v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[8 * n + k] = v[k];
+  }
+  if (cols >= 128) return hadamard_lanes<8 * N>(x, lane, cols == 128 ? 4 : cols == 256 ? 5 : 6);
+  const float s0 = (lane & 1) ? -1.f : 1.f, s1 = (lane & 2) ? -1.f : 1.f;
+  const float s2 = (lane & 4) ? -1.f : 1.f;
+#pragma unroll
+  for (int e = 0; e < 8 * N; ++e) {
+    if (cols > 8) x[e] = fmaf(x[e], s0, dpp_mov<0xB1>(x[e]));
+    if (cols > 16) x[e] = fmaf(x[e], s1, dpp_mov<0x4E>(x[e]));
+    if (cols > 32) x[e] = fmaf(x[e], s2, dpp_mov<0x1B>(dpp_mov<0x141>(x[e])));
+  }
+}
+
+// Columns c = B a + b: H_B over b, and the 28 x 28 factor over a where C is 28 B (Q in LDS, row a
+// holding the factors of output a). put(c, x, y) takes the results of both elements.
+template <int C, typename Put>
+__device__ __forceinline__ void across_columns(float (&x)[C], float (&y)[C], const float* Q,
+                                               Put put) {
+  if constexpr (C % 28 != 0) {
+    hadamard_reg<C>(x);
+    hadamard_reg<C>(y);
+#pragma unroll
+    for (int c = 0; c < C; ++c) put(c, x[c], y[c]);
+  } else {
+    constexpr int B = C / 28;
+    if constexpr (B == 2) {
+#pragma unroll
+      for (int c = 0; c < C; c += 2) {
+        const float a = x[c], b = x[c + 1], d = y[c], e = y[c + 1];
+        x[c] = a + b, x[c + 1] = a - b, y[c] = d + e, y[c + 1] = d - e;
+      }
+    }
+#pragma unroll 2
+    for (int a = 0; a < 28; ++a) {
+      float u[B] = {}, v[B] = {};
+#pragma unroll
+      for (int k = 0; k < 28; k += 4) {
+        const float4 q = *reinterpret_cast<const float4*>(Q + a * 28 + k);
+        const float f[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int b = 0; b < B; ++b) {
+            u[b] = fmaf(f[i], x[(k + i) * B + b], u[b]);
+            v[b] = fmaf(f[i], y[(k + i) * B + b], v[b]);
+          }
+      }
+#pragma unroll
+      for (int b = 0; b < B; ++b) put(a * B + b, u[b], v[b]);
+    }
+  }
+}
+
+__device__ __forceinline__ void load2(const uint16_t* p, float& a, float& b) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+  a = __uint_as_float(w << 16), b = __uint_as_float(w & 0xFFFF0000u);
+}
+__device__ __forceinline__ void load2(const float* p, float& a, float& b) {
+  const float2 w = *reinterpret_cast<const float2*>(p);
+  a = w.x, b = w.y;
+}
+__device__ __forceinline__ void load8(const uint16_t* p, float* v) {
+  const uint4 w = *reinterpret_cast<const uint4*>(p);
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    v[2 * k] = __uint_as_float(u[k] << 16), v[2 * k + 1] = __uint_as_float(u[k] & 0xFFFF0000u);
+}
+__device__ __forceinline__ void load8(const float* p, float* v) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 4) {
+    const float4 w = *reinterpret_cast<const float4*>(p + k);
+    v[k] = w.x, v[k + 1] = w.y, v[k + 2] = w.z, v[k + 3] = w.w;
+  }
+}
+
+// C: columns of a rotated row (0: not rotated). N: octets a thread ends with.
+template <typename T, int C, int N>
+__global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, int lead) {
+  extern __shared__ __attribute__((aligned(16))) float buf[];  // the row, when rotated
+  __shared__ __attribute__((aligned(16))) float Q[C % 28 == 0 && C ? 784 : 4];
+  __shared__ float red[4];
+  __shared__ int sh[256];
+  const int tid = threadIdx.x, lane = tid & 63;
+  if (int(blockIdx.x) < lead) {
+    if (int(blockIdx.x) < table_blocks) fill_table(A, blockIdx.x);
+    if (int(blockIdx.x) == lead - 1 && A.offsets) list_tiles(A, sh);
+    return;
+  }
+  // The rows of a unit on one XCD (workgroup % 8; lead is a multiple of 8), one after another: a
+  // line of the result holds 8 rows, and is then complete before it leaves that XCD's L2.
+  const int64_t b = int64_t(blockIdx.x) - lead, in = b >> 3;
+  const int64_t row = ((b & 7) + 8 * (in >> 5)) * 32 + (in & 31);
+  if (row >= A.n_rows) return;
+  int expert = 0;
+  if (A.offsets) {
+    expert = expert_of(A.offsets, A.n_experts, row);
+    if (expert < 0) return;
+  }
+  const int d = int(A.d_in);
+  const T* x = static_cast<const T*>(A.x) + row * A.ldx;
+  const float* mul = A.mul ? A.mul + int64_t(expert) * d : nullptr;
+  float v[8 * N];
+  if constexpr (C > 0) {
+    const int cols = A.turn.cols;
+    if constexpr (C % 28 == 0) {
+      const float* q = A.q28 + int64_t(expert) * 784;
+      for (int i = tid; i < 784; i += 256) Q[i] = q[i];
+      __syncthreads();
+    }
+    const int p = 2 * tid;
+    if (p < cols) {
+      float u[C], w[C];
+#pragma unroll
+      for (int c = 0; c < C; ++c) load2(x + c * cols + p, u[c], w[c]);
+      if (mul) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const float2 f = *reinterpret_cast<const float2*>(mul + c * cols + p);
+          u[c] *= f.x, w[c] *= f.y;
+        }
+      }
+      across_columns<C>(u, w, Q, [&](int c, float a, float b) {
+        *reinterpret_cast<float2*>(buf + c * cols + p) = make_float2(a, b);
+      });
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int j = 8 * (tid + 256 * n);
+      float o[8] = {};
+      if (j < d) load8(buf + j, o);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[8 * n + k] = o[k];
+    }
+    inside_column<N>(v, lane, cols);
+  } else {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int j = 8 * (tid + 256 * n);
+      float o[8] = {};
+      if (j < d) {
+        load8(x + j, o);
+        if (mul) {
+          float f[8];
+          load8(mul + j, f);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) o[k] *= f[k];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[8 * n + k] = o[k];
+    }
+  }
+  // the row's largest value to [2^7, 2^8)
+  float mx = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8 * N; ++k) mx = fmaxf(mx, fabsf(v[k]));
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  if (lane == 0) red[tid >> 6] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])) * A.turn.norm;
+  const int e = int(__float_as_uint(mx) >> 23) - 127;
+  const int ue = mx > 0.f && e < 128 ? clampi(e - 7, -100, 100) : 0;
+  const float up = pow2f(-ue) * A.turn.norm;
+  if (tid == 0) A.row_unit[row] = pow2f(ue);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int j = 8 * (tid + 256 * n);
+    float o[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      o[k] = v[8 * n + k] * up;
+      asm("" : "+v"(o[k]));  // both planes from the one rounded product (a multiplication merged
+    }                        // into one conversion only would round the planes' sum twice)
+    // octet oc of its chunk of 32 columns is step oc of the codes, in the order of chunk_col; with
+    // 2 bits a step takes four columns of either of two octets, which lie in neighbouring lanes
+    float t[8];
+    if (A.bits == 2) {
+      const bool odd = lane & 1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float got = dpp_mov<0xB1>(odd ? o[k] : o[4 + k]);
+        t[2 * k] = odd ? got : o[k];
+        t[2 * k + 1] = odd ? o[4 + k] : got;
+      }
+    } else if (A.bits == 8) {
+      t[0] = o[0], t[1] = o[2], t[2] = o[1], t[3] = o[3];
+      t[4] = o[4], t[5] = o[6], t[6] = o[5], t[7] = o[7];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) t[2 * k] = o[k], t[2 * k + 1] = o[4 + k];
+    }
+    if (j >= d) continue;
+    f16x8_t hi, lo;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) hi[k] = _Float16(t[k]), lo[k] = _Float16(t[k] - float(hi[k]));
+    const int ks = (j >> 7) * 8 + ((j >> 5) & 1) * 4 + ((j >> 3) & 3), h = (j >> 6) & 1;
+    uint16_t* to = A.xf + (((row >> 5) * (d / 16) + ks) * 64 + (row & 31) + 32 * h) * 8;
+    *reinterpret_cast<f16x8_t*>(to) = hi;
+    if (A.planes == 2) *reinterpret_cast<f16x8_t*>(to + A.plane) = lo;
+  }
+}
+
+__device__ __forceinline__ float activate(float z, int act) {
+  switch (act) {
+    case KRONQ_ACT_RELU:
+      return z < 0.f ? 0.f : z;  // (NaN stays)
+    case KRONQ_ACT_GELU:
+      return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case KRONQ_ACT_SILU:
+      return z / (1.f + expf(-z));
+    default:
+      return z;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ float load1(const void* p, int64_t i) {
+  if constexpr (sizeof(T) == 2) return bf16_f32(static_cast<const uint16_t*>(p)[i]);
+  return static_cast<const float*>(p)[i];
+}
+
+template <typename T>
+__device__ __forceinline__ void store1(void* p, int64_t i, float v) {
+  if constexpr (sizeof(T) == 2)
+    static_cast<uint16_t*>(p)[i] = f32_bf16(v);
+  else
+    static_cast<float*>(p)[i] = v;
+}
+
+// bias, activation and residual of element j of a row
+template <typename T>
+__device__ __forceinline__ float finish(const LinearOut& A, int64_t row, int expert, int j, float v) {
+  const int64_t at = int64_t(expert) * A.d_out + j;
+  if (A.mul) v *= A.mul[at];
+  if (A.bias) v += A.bias[at];
+  v = activate(v, A.act);
+  if (A.residual) v += load1<T>(A.residual, row * A.ldr + j);
+  return v;
+}
+
+// eight neighbours of y', summed over the splits
+__device__ __forceinline__ void sum8(const LinearOut& A, int64_t row, int j, float* v) {
+  const float* p = A.part + row * A.ld + j;
+  load8(p, v);
+#pragma unroll 4
+  for (int s = 1; s < A.splits; ++s) {
+    float w[8];
+    load8(p + s * A.stride, w);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += w[k];
+  }
+}
+
+// C columns of a rotated row of whole octets
+template <typename T, int C>
+__global__ __launch_bounds__(256) void linear_out(LinearOut A) {
+  extern __shared__ __attribute__((aligned(16))) float buf[];  // the row
+  __shared__ __attribute__((aligned(16))) float Q[C % 28 == 0 ? 784 : 4];
+  constexpr int N = C >= 4 ? C / 4 : 1;
+  const int tid = threadIdx.x, lane = tid & 63, d = int(A.d_out), cols = A.turn.cols;
+  const int64_t row = blockIdx.x;
+  int expert = 0;
+  if (A.offsets) {
+    expert = expert_of(A.offsets, A.n_experts, row);
+    if (expert < 0) return;
+  }
+  if constexpr (C % 28 == 0) {  // the transposed factor
+    const float* q = A.q28 + int64_t(expert) * 784;
+    for (int i = tid; i < 784; i += 256) Q[(i % 28) * 28 + i / 28] = q[i];
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int j = 8 * (tid + 256 * n);
+    float v[8] = {};
+    if (j < d) sum8(A, row, j, v);
+    inside_column<1>(v, lane, cols);
+    if (j < d) {
+      *reinterpret_cast<float4*>(buf + j) = make_float4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<float4*>(buf + j + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  }
+  __syncthreads();
+  const int p = 2 * tid;
+  if (p >= cols) return;
+  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm;
+  float u[C], w[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const float2 f = *reinterpret_cast<const float2*>(buf + c * cols + p);
+    u[c] = f.x, w[c] = f.y;
+  }
+  across_columns<C>(u, w, Q, [&](int c, float a, float b) {
+    const int j = c * cols + p;
+    a = finish<T>(A, row, expert, j, a * up);
+    b = finish<T>(A, row, expert, j + 1, b * up);
+    store1<T>(A.y, row * A.ldy + j, a);
+    store1<T>(A.y, row * A.ldy + j + 1, b);
+  });
+}
+
+// Rows without a transform, and transforms whose columns are shorter than an octet (cols: 1, 2 or 4
+// elements in each of 28 or fewer columns: the dense product).
+template <typename T>
+__global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
+  __shared__ float small[128];
+  const int tid = threadIdx.x, d = int(A.d_out);
+  const int64_t row = blockIdx.x;
+  int expert = 0;
+  if (A.offsets) {
+    expert = expert_of(A.offsets, A.n_experts, row);
+    if (expert < 0) return;
+  }
+  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm;
+  const float* p = A.part + row * A.ld;
+  for (int j = tid; j < d; j += 256) {
+    float v = p[j];
+    for (int s = 1; s < A.splits; ++s) v += p[s * A.stride + j];
+    if (A.turn.rotate)
+      small[j] = v;  // (d <= 28 * 4)
+    else
+      store1<T>(A.y, row * A.ldy + j, finish<T>(A, row, expert, j, v * up));
+  }
+  if (!A.turn.rotate) return;
+  __syncthreads();
+  const float* q = A.q28 + int64_t(expert) * 784;
+  for (int j = tid; j < d; j += 256) {
+    const int a = j / A.turn.m, b = j % A.turn.m;
+    float v = 0.f;
+    for (int k = 0; k < d; ++k) {
+      const float h = (__popc(unsigned(b & (k % A.turn.m))) & 1) ? -small[k] : small[k];
+      v = fmaf(A.turn.has28 ? q[(k / A.turn.m) * 28 + a] : 1.f, h, v);
+    }
+    store1<T>(A.y, row * A.ldy + j, finish<T>(A, row, expert, j, v * up));
+  }
+}
+
+template <typename T>
+int in_typed(const LinearIn& a, hipStream_t s) {
+  const int64_t table_blocks = a.table ? cdiv(a.w_rows, 8) : 0;
+  const int64_t lead = cdiv(table_blocks + (a.offsets ? 1 : 0), 8) * 8;
+  const dim3 grid(static_cast<unsigned>(lead + cdiv(a.n_rows, 256) * 256));
+#define KQ_IN(C_, N_)                                                                              \
+  launch("linear_in", linear_in<T, C_, N_>, grid, dim3(256), C_ ? size_t(a.d_in) * 4 : 0, s, a, \
+         int(table_blocks), int(lead))
+  if (!a.turn.rotate) {
+    const int64_t n = cdiv(a.d_in, 2048);
+    return n <= 1 ? KQ_IN(0, 1) : n <= 2 ? KQ_IN(0, 2) : n <= 4 ? KQ_IN(0, 4) : n <= 8 ? KQ_IN(0, 8)
+                                                                                  : KQ_IN(0, 16);
+  }
+  switch (a.d_in / a.turn.cols) {
+    case 1:
+      return KQ_IN(1, 1);
+    case 2:
+      return KQ_IN(2, 1);
+    case 4:
+      return KQ_IN(4, 1);
+    case 8:
+      return KQ_IN(8, 2);
+    case 16:
+      return KQ_IN(16, 4);
+    case 32:
+      return KQ_IN(32, 8);
+    case 64:
+      return KQ_IN(64, 16);
+    case 28:
+      return KQ_IN(28, 7);
+    default:
+      return KQ_IN(56, 14);
+  }
+#undef KQ_IN
+}
+
+template <typename T>
+int out_typed(const LinearOut& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(a.n_rows));
+  if (!a.turn.rotate || a.turn.cols < 8)
+    return launch("linear_out", linear_out_any<T>, grid, dim3(256), 0, s, a);
+#define KQ_OUT(C_) \
+  launch("linear_out", linear_out<T, C_>, grid, dim3(256), size_t(a.d_out) * 4, s, a)
+  switch (a.d_out / a.turn.cols) {
+    case 1:
+      return KQ_OUT(1);
+    case 2:
+      return KQ_OUT(2);
+    case 4:
+      return KQ_OUT(4);
+    case 8:
+      return KQ_OUT(8);
+    case 16:
+      return KQ_OUT(16);
+    case 32:
+      return KQ_OUT(32);
+    case 64:
+      return KQ_OUT(64);
+    case 28:
+      return KQ_OUT(28);
+    default:
+      return KQ_OUT(56);
+  }
+#undef KQ_OUT
+}
+
+}  // namespace
+
+LinearTurn linear_turn(int64_t d, bool rotate) {
+  const RotDim rd = rot_dim(d);
+  LinearTurn t{rotate, rotate && rd.has28, 1, 1, 1.f};
+  if (rotate) {
+    t.m = int(rd.m), t.cols = t.m < 512 ? t.m : 512;
+    t.norm = float(1.0 / std::sqrt(double(rd.m)));
+  }
+  return t;
+}
+
+int linear_in_launch(const LinearIn& a, hipStream_t s) {
+  return a.x_dtype == KRONQ_BF16 ? in_typed<uint16_t>(a, s) : in_typed<float>(a, s);
+}
+int linear_out_launch(const LinearOut& a, hipStream_t s) {
+  return a.y_dtype == KRONQ_BF16 ? out_typed<uint16_t>(a, s) : out_typed<float>(a, s);
+}
+
+}  // namespace kq
