@@ -12,6 +12,24 @@ struct LinearTile {
   int expert, unit, lo, hi;
 };
 
+// Many rows: the outputs are cut into items of a row tile and 256 rows of W, tile after tile, which
+// `workers` workgroups share: whole items in full rounds, and the groups of columns of the items left
+// over in equal parts, `per` groups a worker in item order. So the last round is as full as the others;
+// a worker that begins inside an item keeps that part in a place of its own, for linear_out to add.
+struct LinearDeal {
+  int full, per;  // rounds of whole items; groups of the rest per worker
+};
+__host__ __device__ inline LinearDeal linear_deal(int items, int ng, int workers) {
+  const int full = items / workers, rest = items - full * workers;
+  int per = (rest * ng + workers - 1) / workers;
+  // few groups a worker are mostly start and end, and a rest that nearly fills a round gains less
+  // than its parts cost to write and read again
+  if (per < 2) per = 2;
+  if (per * 10 > ng * 9) per = ng;
+  return LinearDeal{full, per};
+}
+constexpr int LINEAR_BLOCK = 256;  // rows of W of an item
+
 // Column (of a chunk of 32) of element i of step jj of a lane's eight codes, in the order in which
 // the codes of a packed chunk are spread to pairs of fp16.
 __host__ __device__ inline int chunk_col(int bits, int jj, int i) {
@@ -53,14 +71,24 @@ struct LinearIn {
   int n_experts, nt;
   int64_t max_tiles;
   LinearTile* tiles;
+  int2* first;     // [n_experts] first tile and first unit of each expert
 };
 int linear_in_launch(const LinearIn& a, hipStream_t s);
 
-// y = act(diag(mul_out) T_out y' + bias) + residual with y' the sum of the splits
+// y = act(diag(mul_out) T_out y' + bias) + residual
 struct LinearOut {
-  const float* part;      // [split][row][ld]
-  int64_t ld, stride;     // of a row and a split
+  // y': the sum of the splits, fp32 [split][row][ld]; or dealt (workers > 0): [row][ld] and the parts
+  // that workers keep, [worker][32 nt][LINEAR_BLOCK], both fp16 to be multiplied by w_unit (with
+  // w_unit) or fp32
+  const void* part;
+  int64_t ld, stride;
   int splits;
+  int workers, ng, nt, row_blocks, items;  // items without offsets
+  const void* kept;
+  const float* w_unit;
+  const LinearTile* tiles;
+  const int2* first;
+  float unit;             // of everything
   const float* row_unit;  // or null (1)
   int64_t n_rows, d_out;
   const float *mul, *q28;

@@ -57,8 +57,10 @@ struct MmArgs {
   const Tile* tiles;  // null: one layer, unit tiles in order
   int64_t n_rows;
   int row_blocks, splits, per;  // groups per split
-  float* part;        // [split][row][ld]
+  void* part;         // linear_mfma: fp32 [split][row][ld]; linear_ring: [row][ld]
   int64_t ld;
+  void* kept;         // linear_ring: [worker][32 NT][LINEAR_BLOCK]
+  float down;         // of fp16 results
 };
 
 __device__ __forceinline__ f16x2_t h2(uint32_t v) { return __builtin_bit_cast(f16x2_t, v); }
@@ -204,7 +206,7 @@ __global__ __launch_bounds__(256) void linear_mfma(MmArgs A) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][r] = fmaf(sc, sum[i][r], acc[i][r]);
   }
-  float* part = A.part + int64_t(split) * A.n_rows * A.ld;
+  float* part = static_cast<float*>(A.part) + int64_t(split) * A.n_rows * A.ld;
   if (n >= A.d_out) return;
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
@@ -249,8 +251,10 @@ __device__ __forceinline__ Chunk<BITS> load_chunk(const uint32_t* p) {
 // lane's codes) of NT units in PLANES planes, NT PLANES = 4 pieces of 4 KB of which each wave brings
 // one straight to LDS, in fragment order as it stands, through a ring of four stages. One barrier a
 // stage, in its middle: it publishes the next stage and frees the buffer of the one before, which the
-// loads of three stages on then fill; operands are read one step of 16 columns ahead. Two workgroups per CU (64 KB of LDS and 256 registers a lane each), so that
-// one wave's spreading of codes runs beside the other's matrix instructions.
+// loads of three stages on then fill; operands are read one step of 16 columns ahead. Two workgroups
+// per CU (64 KB of LDS and 256 registers a lane each), so that one wave's spreading of codes runs
+// beside the other's matrix instructions. Scaled results leave as fp16 (linear_out multiplies by the
+// units of the rows of W).
 template <int BITS, int NT, int PLANES>
 __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
   constexpr int RT = 2, STAGE = 4 * 1024, R = 4;  // (dwords)
@@ -258,172 +262,183 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
   static_assert(NT * PLANES == 4, "one piece of a stage per wave");
   __shared__ __attribute__((aligned(16))) uint32_t lds[R * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // An XCD (workgroup % 8) takes every eighth pair of a row tile and a split, all blocks of W one
-  // after another: the x' of a tile is read through one L2, where its workgroups share it.
-  const int item = int(blockIdx.x & 7) + 8 * int((blockIdx.x >> 3) / A.row_blocks);
-  const int rb = int((blockIdx.x >> 3) % A.row_blocks);
-  const int ti = item / A.splits, split = item % A.splits;
-  Tile t;
-  if (A.tiles) {
-    if (ti >= A.tiles[0].expert) return;
-    t = A.tiles[1 + ti];
-  } else {
-    t = Tile{0, ti * NT, 0, int(A.n_rows)};
-    if (t.unit * 32 >= t.hi) return;
-  }
-  const int g0 = split * A.per, g1 = g0 + A.per < A.ng ? g0 + A.per : A.ng;
-  const int64_t n0 = int64_t(rb) * (128 * RT) + wave * (32 * RT);
-  const int last = (t.hi - 1) >> 5;  // last unit
-  const int nst = 2 * (g1 - g0);
-  const int un = t.unit + wave / PLANES;
-  // (buffer loads: beside global_load_lds the compiler waits for every outstanding load before it
-  // uses one that went to a register)
-  const uint16_t* const piece = A.xf + (PLANES == 2 ? (wave & 1) * A.plane : 0) +
-                                (un < last ? un : last) * int64_t(A.ng) * 4096;
-  const auto src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(piece), 0, A.ng * 8192,
-                                                     0x00027000);
-  auto issue = [&](int st) {  // past the end: the last stage again, never read
-    const int at = (2 * g0 + (st < nst ? st : nst - 1)) * 4096;
-    uint32_t* dst = lds + (st & (R - 1)) * STAGE + wave * 1024;
+  // Workers that share an XCD (workgroup % 8) stand next to one another in the deal, so that the x'
+  // of a tile is read through one L2, by all blocks of W at about the same time.
+  const int W = int(gridDim.x), id = int(blockIdx.x & 7) * (W >> 3) + int(blockIdx.x >> 3);
+  const int ntiles = A.tiles ? A.tiles[0].expert : int(cdiv(A.n_rows, 32 * NT));
+  const int items = ntiles * A.row_blocks;
+  const LinearDeal deal = linear_deal(items, A.ng, W);
+  const int rest = items - deal.full * W;
+  int round = 0, ua = id * deal.per;  // next group of the rest
+  const int ub = ua + deal.per < rest * A.ng ? ua + deal.per : rest * A.ng;
+  for (;;) {
+    int item, g0 = 0, g1 = A.ng;
+    if (round < deal.full) {
+      item = round++ * W + id;
+    } else if (ua < ub) {
+      const int r = ua / A.ng;
+      item = deal.full * W + r;
+      g0 = ua - r * A.ng;
+      g1 = g0 + (ub - ua) < A.ng ? g0 + (ub - ua) : A.ng;
+      ua += g1 - g0;
+    } else {
+      break;
+    }
+    const int rb = item % A.row_blocks, ti = item / A.row_blocks;
+    const Tile t = A.tiles ? A.tiles[1 + ti] : Tile{0, ti * NT, 0, int(A.n_rows)};
+    const int64_t n0 = int64_t(rb) * (128 * RT) + wave * (32 * RT);
+    const int last = (t.hi - 1) >> 5;  // last unit
+    const int nst = 2 * (g1 - g0);
+    const int un = t.unit + wave / PLANES;
+    // (buffer loads: beside global_load_lds the compiler waits for every outstanding load before it
+    // uses one that went to a register)
+    const uint16_t* const piece = A.xf + (PLANES == 2 ? (wave & 1) * A.plane : 0) +
+                                  (un < last ? un : last) * int64_t(A.ng) * 4096;
+    const auto src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(piece), 0, A.ng * 8192,
+                                                       0x00027000);
+    auto issue = [&](int st) {  // past the end: the last stage again, never read
+      const int at = (2 * g0 + (st < nst ? st : nst - 1)) * 4096;
+      uint32_t* dst = lds + (st & (R - 1)) * STAGE + wave * 1024;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, KQ_LDS(dst + q * 256), 16, lane * 16,
-                                               at + q * 1024, 0, 0);
-  };
-  const uint32_t* wp[RT];
-  int64_t wr[RT];
-#pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    const int64_t n = n0 + 32 * i + (lane & 31);
-    wr[i] = int64_t(t.expert) * A.d_out + (n < A.d_out ? n : A.d_out - 1);
-    wp[i] = A.packed + wr[i] * A.ldp + (int64_t(g0) * 4 + (lane >> 5) * 2) * BITS;
-  }
-  Chunk<BITS> cw[2][RT];
-  uint32_t sz1[RT];  // of the next group
-  float sc[RT], sc1[RT];
-  auto codes = [&](int st, int h) {  // h = st & 1
-    st = st < nst ? st : nst - 1;
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-      cw[h][i] = load_chunk<BITS>(wp[i] + int64_t(st >> 1) * 4 * BITS + (st & 1) * BITS);
-  };
-  auto params = [&](int gi) {  // of the group gi of this range
-    const int g = g0 + gi < g1 ? g0 + gi : g1 - 1;
+      for (int q = 0; q < 4; ++q)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, KQ_LDS(dst + q * 256), 16, lane * 16,
+                                                 at + q * 1024, 0, 0);
+    };
+    const uint32_t* wp[RT];
+    int64_t wr[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-      if constexpr (SCALED) {
-        sz1[i] = A.table[int64_t(g) * A.w_rows + wr[i]];
-      } else {
-        const int64_t at = wr[i] * A.ldsz + unsigned(g) / unsigned(A.gpq);
-        sc1[i] = A.scales[at];
-        sz1[i] = __float_as_uint(A.zeros[at]);
-      }
+      const int64_t n = n0 + 32 * i + (lane & 31);
+      wr[i] = int64_t(t.expert) * A.d_out + (n < A.d_out ? n : A.d_out - 1);
+      wp[i] = A.packed + wr[i] * A.ldp + (int64_t(g0) * 4 + (lane >> 5) * 2) * BITS;
     }
-  };
-  f32x16_t acc[NT][RT] = {}, sum[SCALED ? 1 : NT][SCALED ? 1 : RT] = {};
-  params(0);
-  codes(0, 0);
-  __builtin_amdgcn_sched_barrier(0);
+    Chunk<BITS> cw[2][RT];
+    uint32_t sz1[RT];  // of the next group
+    float sc[RT], sc1[RT];
+    auto codes = [&](int st, int h) {  // h = st & 1
+      st = st < nst ? st : nst - 1;
 #pragma unroll
-  for (int st = 0; st < 3; ++st) issue(st);
-  u32x4_t a[2][4];
-  auto frags = [&](int st, int q) {
-    const uint32_t* buf = lds + (st & (R - 1)) * STAGE + lane * 4 + q * 256;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a[q & 1][i] = *reinterpret_cast<const u32x4_t*>(buf + i * 1024);
-  };
-  uint32_t z[RT];
-  auto stage = [&](int st, auto hc) {
-    constexpr int h = decltype(hc)::value;
-    codes(st + 1, h ^ 1);
-    if constexpr (h == 0) {
+      for (int i = 0; i < RT; ++i)
+        cw[h][i] = load_chunk<BITS>(wp[i] + int64_t(st >> 1) * 4 * BITS + (st & 1) * BITS);
+    };
+    auto params = [&](int gi) {  // of the group gi of this range
+      const int g = g0 + gi < g1 ? g0 + gi : g1 - 1;
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
-        z[i] = sz1[i], sc[i] = sc1[i];
-        if constexpr (!SCALED) {
-          const _Float16 nz = _Float16(-1024.f - __uint_as_float(sz1[i]));
-          z[i] = u2(f16x2_t{nz, nz});
+        if constexpr (SCALED) {
+          sz1[i] = A.table[int64_t(g) * A.w_rows + wr[i]];
+        } else {
+          const int64_t at = wr[i] * A.ldsz + unsigned(g) / unsigned(A.gpq);
+          sc1[i] = A.scales[at];
+          sz1[i] = __float_as_uint(A.zeros[at]);
         }
       }
-      params((st >> 1) + 1);
-    }
+    };
+    f32x16_t acc[NT][RT] = {}, sum[SCALED ? 1 : NT][SCALED ? 1 : RT] = {};
+    params(0);
+    codes(0, 0);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (q == 2) {
-        // the next stage's loads have landed (those of the one after it may be out, and what this
-        // wave has requested of codes since)
-        wait_vm<8>();
-        __builtin_amdgcn_s_barrier();
-        issue(st + 3);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      frags(q < 3 ? st : st + 1, (q + 1) & 3);
-      u32x4_t b[RT];
+    for (int st = 0; st < 3; ++st) issue(st);
+    u32x4_t a[2][4];
+    auto frags = [&](int st, int q) {
+      const uint32_t* buf = lds + (st & (R - 1)) * STAGE + lane * 4 + q * 256;
 #pragma unroll
-      for (int k = 0; k < RT; ++k)
-        b[k] = SCALED ? spread<BITS>(cw[h][k].w, q, z[k]) : spread_int<BITS>(cw[h][k].w, q, z[k]);
+      for (int i = 0; i < 4; ++i) a[q & 1][i] = *reinterpret_cast<const u32x4_t*>(buf + i * 1024);
+    };
+    uint32_t z[RT];
+    auto stage = [&](int st, auto hc) {
+      constexpr int h = decltype(hc)::value;
+      codes(st + 1, h ^ 1);
+      if constexpr (h == 0) {
 #pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int k = 0; k < RT; ++k) {
-          if constexpr (SCALED) {
-            acc[i][k] = mfma(a[q & 1][i], b[k], acc[i][k]);
-          } else {
-            sum[i][k] = mfma(a[q & 1][2 * i + 1], b[k], sum[i][k]);
-            sum[i][k] = mfma(a[q & 1][2 * i], b[k], sum[i][k]);
+        for (int i = 0; i < RT; ++i) {
+          z[i] = sz1[i], sc[i] = sc1[i];
+          if constexpr (!SCALED) {
+            const _Float16 nz = _Float16(-1024.f - __uint_as_float(sz1[i]));
+            z[i] = u2(f16x2_t{nz, nz});
           }
         }
-      __builtin_amdgcn_sched_barrier(0);  // (else every step's operands are read at once, and spill)
-    }
-    if constexpr (!SCALED) {
-      if constexpr (h == 1) {
+        params((st >> 1) + 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (q == 2) {
+          // the next stage's loads have landed (those of the one after it may be out, and what this
+          // wave has requested of codes since)
+          wait_vm<8>();
+          __builtin_amdgcn_s_barrier();
+          issue(st + 3);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        frags(q < 3 ? st : st + 1, (q + 1) & 3);
+        u32x4_t b[RT];
+#pragma unroll
+        for (int k = 0; k < RT; ++k)
+          b[k] = SCALED ? spread<BITS>(cw[h][k].w, q, z[k]) : spread_int<BITS>(cw[h][k].w, q, z[k]);
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
-          for (int k = 0; k < RT; ++k)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              acc[i][k][r] = fmaf(sc[k], sum[i][k][r], acc[i][k][r]);
-              sum[i][k][r] = 0.f;
+          for (int k = 0; k < RT; ++k) {
+            if constexpr (SCALED) {
+              acc[i][k] = mfma(a[q & 1][i], b[k], acc[i][k]);
+            } else {
+              sum[i][k] = mfma(a[q & 1][2 * i + 1], b[k], sum[i][k]);
+              sum[i][k] = mfma(a[q & 1][2 * i], b[k], sum[i][k]);
             }
+          }
+        __builtin_amdgcn_sched_barrier(0);  // (else every step's operands are read at once, and spill)
       }
+      if constexpr (!SCALED) {
+        if constexpr (h == 1) {
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int k = 0; k < RT; ++k)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                acc[i][k][r] = fmaf(sc[k], sum[i][k][r], acc[i][k][r]);
+                sum[i][k][r] = 0.f;
+              }
+        }
+      }
+    };
+    wait_vm<8>();
+    __builtin_amdgcn_s_barrier();
+    frags(0, 0);
+    for (int st = 0; st < nst; st += 2) {
+      stage(st, std::integral_constant<int, 0>{});
+      stage(st + 1, std::integral_constant<int, 1>{});
     }
-  };
-  wait_vm<8>();
-  __builtin_amdgcn_s_barrier();
-  frags(0, 0);
-  for (int st = 0; st < nst; st += 2) {
-    stage(st, std::integral_constant<int, 0>{});
-    stage(st + 1, std::integral_constant<int, 1>{});
-  }
-  wait_vm<0>();  // (loads past the end still write to LDS)
-  float* part = A.part + int64_t(split) * A.n_rows * A.ld;
+    wait_vm<0>();  // (loads past the end still write to LDS)
+    __builtin_amdgcn_s_barrier();
+    // a worker that began inside an item keeps its part
+    using Part = std::conditional_t<SCALED, _Float16, float>;
+    const int64_t ld = g0 > 0 ? LINEAR_BLOCK : A.ld;
+    Part* const part =
+        g0 > 0 ? static_cast<Part*>(A.kept) + (int64_t(id) * NT - t.unit) * 32 * LINEAR_BLOCK -
+                     rb * LINEAR_BLOCK
+               : static_cast<Part*>(A.part);
 #pragma unroll
-  for (int k = 0; k < RT; ++k) {
-    const int64_t n = n0 + 32 * k + (lane & 31);
-    const float unit = SCALED ? A.w_unit[wr[k]] : 1.f;
+    for (int k = 0; k < RT; ++k) {
+      const int64_t n = n0 + 32 * k + (lane & 31);
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      const int mu = (t.unit + i) * 32, m0 = mu + 4 * (lane >> 5);
-      float* p = part + int64_t(m0) * A.ld + n;
-      if (mu >= t.lo && mu + 32 <= t.hi) {  // (uniform) every row of the unit is the tile's
+      for (int i = 0; i < NT; ++i) {
+        const int mu = (t.unit + i) * 32, m0 = mu + 4 * (lane >> 5);
+        Part* p = part + int64_t(m0) * ld + n;
+        const bool whole = mu >= t.lo && mu + 32 <= t.hi;  // (uniform) every row of it is the tile's
         if (n < A.d_out) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            *p = acc[i][k][r] * unit;
-            p += (r & 3) == 3 ? 5 * A.ld : A.ld;
+            const int m = m0 + 8 * (r >> 2) + (r & 3);
+            const float v = SCALED ? acc[i][k][r] * A.down : acc[i][k][r];
+            if (whole || (m >= t.lo && m < t.hi)) *p = Part(v);
+            p += (r & 3) == 3 ? 5 * ld : ld;
           }
         }
-      } else if (n < A.d_out) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int m = m0 + 8 * (r >> 2) + (r & 3);
-          if (m >= t.lo && m < t.hi) *p = acc[i][k][r] * unit;
-          p += (r & 3) == 3 ? 5 * A.ld : A.ld;
-        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
   }
 }
@@ -433,8 +448,9 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
 constexpr int64_t GEMV_ROWS = 4, GEMV_INPUTS = 32768;
 
 struct Plan {
-  int planes, nt, splits, per;
+  int planes, nt, splits, per, workers;
   bool ring, scaled;
+  float down;
   int64_t tiles, row_blocks;
 };
 
@@ -446,7 +462,14 @@ Plan make_plan(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts, i
   p.scaled = p.ring && p.planes == 1;
   p.nt = p.ring ? 4 / p.planes : per_expert > 32 ? 2 : 1;
   p.tiles = n_experts == 1 ? cdiv(n_rows, 32 * p.nt) : most_tiles(n_rows, n_experts, p.nt);
-  p.row_blocks = cdiv(d_out, p.ring ? 256 : 128);
+  p.row_blocks = cdiv(d_out, p.ring ? LINEAR_BLOCK : 128);
+  p.splits = 1, p.per = int(ng), p.workers = 0, p.down = 1.f;
+  if (p.ring) {
+    p.workers = device_cus() / 4 * 8;  // two per CU
+    // fp16 results: below 2^8 (x') times 2.5 (|c - z| < 1280 of at most 2^-9) times d_in
+    while (p.scaled && 640.f * float(d_in) * p.down > 65000.f) p.down *= 0.5f;
+    return p;
+  }
   const int64_t wgs = p.tiles * p.row_blocks;
   int64_t s = wgs < 512 ? 512 / wgs : 1;
   if (s > ng) s = ng;
@@ -458,9 +481,11 @@ Plan make_plan(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts, i
 
 struct Ws {
   uint16_t* xf;
-  float *row_unit, *w_unit, *part;
+  float *row_unit, *w_unit;
+  char *part, *kept;
   uint32_t* table;
   Tile* tiles;
+  int2* first;
   size_t bytes;
 };
 
@@ -470,11 +495,14 @@ Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, i
   Ws w;
   w.xf = cv.take<uint16_t>(size_t(p.planes) * size_t(cdiv(n_rows, 32) * 32) * size_t(d_in));
   w.row_unit = cv.take<float>(size_t(n_rows));
-  w.part = cv.take<float>(size_t(p.splits) * size_t(n_rows) * size_t(cdiv(d_out, 8) * 8));
+  const size_t size = p.scaled ? 2 : 4;  // of a product
+  w.part = cv.take<char>(size_t(p.splits) * size_t(n_rows) * size_t(cdiv(d_out, 8) * 8) * size);
+  w.kept = cv.take<char>(size_t(p.workers) * size_t(32 * p.nt) * LINEAR_BLOCK * size);
   const size_t w_rows = p.scaled ? size_t(n_experts) * size_t(d_out) : 0;
   w.w_unit = cv.take<float>(w_rows);
   w.table = cv.take<uint32_t>(w_rows * size_t(d_in / 128));
   w.tiles = cv.take<Tile>(grouped ? size_t(p.tiles) + 1 : 0);
+  w.first = cv.take<int2>(grouped ? size_t(n_experts) : 0);
   w.bytes = align256(cv.used) + 256;
   return w;
 }
@@ -482,7 +510,7 @@ Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, i
 template <int BITS>
 int launch_mm(const MmArgs& a, const Plan& p, hipStream_t s) {
   if (p.ring) {
-    const dim3 grid(static_cast<unsigned>(8 * cdiv(p.tiles * p.splits, 8) * p.row_blocks));
+    const dim3 grid(static_cast<unsigned>(p.workers));
     return p.planes == 1
                ? launch("linear_ring", linear_ring<BITS, 4, 1>, grid, dim3(256), 0, s, a)
                : launch("linear_ring", linear_ring<BITS, 2, 2>, grid, dim3(256), 0, s, a);
@@ -520,7 +548,7 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
     KQ_TRY(online_product_launch(j.packed, j.ldp, j.scales, j.zeros, j.ldsz, j.bits, j.group,
                                  j.d_out, j.d_in, j.mul_in, j.q28_in, j.flags, j.x, j.x_dtype,
                                  j.ldx, j.n_rows, ws, &yr, s));
-    o.part = yr, o.ld = j.d_out, o.splits = 1;
+    o.part = yr, o.ld = j.d_out, o.splits = 1, o.unit = 1.f;
     return linear_out_launch(o, s);
   }
   const Plan p = make_plan(j.d_out, j.d_in, j.n_rows, j.n_experts, j.y_dtype);
@@ -534,7 +562,7 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
   a.scales = j.scales, a.zeros = j.zeros, a.ldsz = j.ldsz;
   a.gpq = j.group / 128, a.ng = int(j.d_in / 128), a.w_rows = j.n_experts * j.d_out;
   a.offsets = j.offsets, a.n_experts = int(j.n_experts), a.nt = p.nt;
-  a.max_tiles = p.tiles, a.tiles = w.tiles;
+  a.max_tiles = p.tiles, a.tiles = w.tiles, a.first = w.first;
   KQ_TRY(linear_in_launch(a, s));
   MmArgs m{};
   m.packed = j.packed, m.ldp = j.ldp, m.d_out = j.d_out, m.w_rows = a.w_rows;
@@ -542,13 +570,16 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
   m.scales = j.scales, m.zeros = j.zeros, m.ldsz = j.ldsz, m.gpq = a.gpq;
   m.tiles = j.offsets ? w.tiles : nullptr, m.n_rows = j.n_rows;
   m.row_blocks = int(p.row_blocks), m.splits = p.splits, m.per = p.per;
-  m.part = w.part, m.ld = cdiv(j.d_out, 8) * 8;
+  m.part = w.part, m.ld = cdiv(j.d_out, 8) * 8, m.kept = w.kept, m.down = p.down;
   KQ_TRY(j.bits == 2   ? launch_mm<2>(m, p, s)
          : j.bits == 3 ? launch_mm<3>(m, p, s)
          : j.bits == 4 ? launch_mm<4>(m, p, s)
                        : launch_mm<8>(m, p, s));
   o.part = w.part, o.ld = m.ld, o.stride = j.n_rows * m.ld, o.splits = p.splits;
-  o.row_unit = w.row_unit;
+  o.row_unit = w.row_unit, o.unit = 1.f / p.down;
+  o.workers = p.workers, o.ng = a.ng, o.nt = p.nt, o.row_blocks = m.row_blocks, o.kept = w.kept;
+  o.items = int(p.tiles * p.row_blocks), o.w_unit = p.scaled ? w.w_unit : nullptr;
+  if (j.offsets) o.tiles = w.tiles, o.first = w.first;
   return linear_out_launch(o, s);
 }
 

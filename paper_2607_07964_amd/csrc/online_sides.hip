@@ -64,13 +64,14 @@ __device__ void list_tiles(const LinearIn& A, int* sh) {
     __syncthreads();
     const int u0 = lo >> 5, nu = hi > lo ? ((hi - 1) >> 5) - u0 + 1 : 0;
     const int k = (nu + A.nt - 1) / A.nt;
-    int sum = k;
+    int sum = k;  // (running over the threads)
     for (int o = 1; o < 256; o <<= 1) {
       sh[tid] = sum;
       __syncthreads();
       if (tid >= o) sum += sh[tid - o];
       __syncthreads();
     }
+    if (e < A.n_experts) A.first[e] = make_int2(base + sum - k, u0);
     for (int i = 0; i < k; ++i) {
       const int64_t at = base + sum - k + i;
       if (at < A.max_tiles) A.tiles[1 + at] = LinearTile{e, u0 + i * A.nt, lo, hi};
@@ -360,21 +361,92 @@ __device__ __forceinline__ float finish(const LinearOut& A, int64_t row, int exp
   return v;
 }
 
-// eight neighbours of y', summed over the splits
-__device__ __forceinline__ void sum8(const LinearOut& A, int64_t row, int j, float* v) {
-  const float* p = A.part + row * A.ld + j;
-  load8(p, v);
-#pragma unroll 4
-  for (int s = 1; s < A.splits; ++s) {
-    float w[8];
-    load8(p + s * A.stride, w);
+__device__ __forceinline__ void load8(const _Float16* p, float* v) {
+  const f16x8_t w = *reinterpret_cast<const f16x8_t*>(p);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += w[k];
-  }
+  for (int k = 0; k < 8; ++k) v[k] = float(w[k]);
 }
 
+// Where a row's products lie. TP: their type.
+template <typename TP>
+struct Products {
+  const LinearOut& A;
+  const TP* p;
+  const float* w_unit;
+  int64_t row;
+  int item0, in_tile, full_items, per;  // dealt
+
+  __device__ __forceinline__ Products(const LinearOut& a, int64_t r, int expert) : A(a), row(r) {
+    p = static_cast<const TP*>(A.part) + row * A.ld;
+    w_unit = A.w_unit ? A.w_unit + int64_t(expert) * A.d_out : nullptr;
+    if (A.workers == 0) return;
+    const int u = int(row >> 5);
+    int ti = u / A.nt, unit = ti * A.nt, items = A.items;
+    if (A.first) {
+      const int2 f = A.first[expert];
+      const int k = (u - f.y) / A.nt;
+      ti = f.x + k, unit = f.y + k * A.nt;
+      items = A.tiles[0].expert * A.row_blocks;
+    }
+    const LinearDeal d = linear_deal(items, A.ng, A.workers);
+    // (offsets that do not ascend give tiles that do not hold the row: kept within the buffers)
+    item0 = clampi(ti, 0, items / A.row_blocks) * A.row_blocks;
+    in_tile = clampi(int(row) - unit * 32, 0, 32 * A.nt - 1);
+    full_items = d.full * A.workers, per = d.per;
+  }
+  // the workers after the first one that hold parts of element j's item: [from, to)
+  __device__ __forceinline__ void parts(int j, int& from, int& to) const {
+    const int r = item0 + j / LINEAR_BLOCK - full_items;
+    from = to = 0;
+    if (r < 0) return;
+    from = r * A.ng / per + 1, to = ((r + 1) * A.ng - 1) / per + 1;
+    to = to < A.workers ? to : A.workers;
+  }
+  __device__ __forceinline__ const TP* kept(int worker, int j) const {
+    return static_cast<const TP*>(A.kept) +
+           (int64_t(worker) * 32 * A.nt + in_tile) * LINEAR_BLOCK + j % LINEAR_BLOCK;
+  }
+  // eight neighbours
+  __device__ __forceinline__ void sum8(int j, float* v) const {
+    load8(p + j, v);
+    float w[8];
+    if (A.workers == 0) {
+#pragma unroll 4
+      for (int s = 1; s < A.splits; ++s) {
+        load8(p + s * A.stride + j, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += w[k];
+      }
+      return;
+    }
+    int from, to;
+    parts(j, from, to);
+    for (int s = from; s < to; ++s) {
+      load8(kept(s, j), w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += w[k];
+    }
+    if (w_unit) {
+      load8(w_unit + j, w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] *= w[k];
+    }
+  }
+  __device__ __forceinline__ float sum1(int j) const {
+    float v = float(p[j]);
+    if (A.workers == 0) {
+      for (int s = 1; s < A.splits; ++s) v += float(p[s * A.stride + j]);
+      return v;
+    }
+    int from, to;
+    parts(j, from, to);
+    for (int s = from; s < to; ++s) v += float(*kept(s, j));
+    return w_unit ? v * w_unit[j] : v;
+  }
+};
+
 // C columns of a rotated row of whole octets
-template <typename T, int C>
+template <typename TP, typename T, int C>
 __global__ __launch_bounds__(256) void linear_out(LinearOut A) {
   extern __shared__ __attribute__((aligned(16))) float buf[];  // the row
   __shared__ __attribute__((aligned(16))) float Q[C % 28 == 0 ? 784 : 4];
@@ -390,11 +462,12 @@ __global__ __launch_bounds__(256) void linear_out(LinearOut A) {
     const float* q = A.q28 + int64_t(expert) * 784;
     for (int i = tid; i < 784; i += 256) Q[(i % 28) * 28 + i / 28] = q[i];
   }
+  const Products<TP> products(A, row, expert);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int j = 8 * (tid + 256 * n);
     float v[8] = {};
-    if (j < d) sum8(A, row, j, v);
+    if (j < d) products.sum8(j, v);
     inside_column<1>(v, lane, cols);
     if (j < d) {
       *reinterpret_cast<float4*>(buf + j) = make_float4(v[0], v[1], v[2], v[3]);
@@ -404,7 +477,7 @@ __global__ __launch_bounds__(256) void linear_out(LinearOut A) {
   __syncthreads();
   const int p = 2 * tid;
   if (p >= cols) return;
-  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm;
+  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
   float u[C], w[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -422,7 +495,7 @@ __global__ __launch_bounds__(256) void linear_out(LinearOut A) {
 
 // Rows without a transform, and transforms whose columns are shorter than an octet (cols: 1, 2 or 4
 // elements in each of 28 or fewer columns: the dense product).
-template <typename T>
+template <typename TP, typename T>
 __global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
   __shared__ float small[128];
   const int tid = threadIdx.x, d = int(A.d_out);
@@ -432,11 +505,10 @@ __global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
     expert = expert_of(A.offsets, A.n_experts, row);
     if (expert < 0) return;
   }
-  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm;
-  const float* p = A.part + row * A.ld;
+  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
+  const Products<TP> products(A, row, expert);
   for (int j = tid; j < d; j += 256) {
-    float v = p[j];
-    for (int s = 1; s < A.splits; ++s) v += p[s * A.stride + j];
+    const float v = products.sum1(j);
     if (A.turn.rotate)
       small[j] = v;  // (d <= 28 * 4)
     else
@@ -492,13 +564,13 @@ int in_typed(const LinearIn& a, hipStream_t s) {
 #undef KQ_IN
 }
 
-template <typename T>
+template <typename TP, typename T>
 int out_typed(const LinearOut& a, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(a.n_rows));
   if (!a.turn.rotate || a.turn.cols < 8)
-    return launch("linear_out", linear_out_any<T>, grid, dim3(256), 0, s, a);
+    return launch("linear_out", linear_out_any<TP, T>, grid, dim3(256), 0, s, a);
 #define KQ_OUT(C_) \
-  launch("linear_out", linear_out<T, C_>, grid, dim3(256), size_t(a.d_out) * 4, s, a)
+  launch("linear_out", linear_out<TP, T, C_>, grid, dim3(256), size_t(a.d_out) * 4, s, a)
   switch (a.d_out / a.turn.cols) {
     case 1:
       return KQ_OUT(1);
@@ -538,7 +610,8 @@ int linear_in_launch(const LinearIn& a, hipStream_t s) {
   return a.x_dtype == KRONQ_BF16 ? in_typed<uint16_t>(a, s) : in_typed<float>(a, s);
 }
 int linear_out_launch(const LinearOut& a, hipStream_t s) {
-  return a.y_dtype == KRONQ_BF16 ? out_typed<uint16_t>(a, s) : out_typed<float>(a, s);
+  if (a.w_unit) return out_typed<_Float16, uint16_t>(a, s);  // (bf16 outputs alone take fp16 products)
+  return a.y_dtype == KRONQ_BF16 ? out_typed<float, uint16_t>(a, s) : out_typed<float, float>(a, s);
 }
 
 }  // namespace kq
