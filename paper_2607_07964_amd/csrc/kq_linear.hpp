@@ -102,6 +102,7 @@ struct LinearOut {
   int64_t ldy;
   const int* offsets;
   int n_experts;
+  bool pairs;             // (set by the launch)
 };
 int linear_out_launch(const LinearOut& a, hipStream_t s);
 

@@ -107,28 +107,123 @@ __device__ void fill_table(const LinearIn& A, int64_t block) {
   if (t == 0) A.w_unit[row] = pow2f(ue);
 }
 
-// Butterfly stages of strides 1, 2, 4 (registers) and 8, 16, ... below cols (lanes) on N octets of
-// neighbours a lane, neighbouring octets in neighbouring lanes. cols is a power of two from 8 on.
-template <int N>
-__device__ __forceinline__ void inside_column(float (&x)[8 * N], int lane, int cols) {
+// The octet of a wave's 64 that a lane holds: lanes 4-7 of each 8 in reverse order, so that the
+// octet 4 further on is the mirrored lane of the 8 (one DPP control) and not two exchanges away.
+__device__ __forceinline__ int octet_of(int lane) { return lane ^ ((lane & 4) ? 3 : 0); }
+// Strides 8 ... 64 are taken as x + s y (y the partner's value, s its sign), one multiply-add with
+// the partner read by DPP: right for the lower element and the negative for the upper one. What is
+// left is this sign of the octet, which the callers multiply by once.
+__device__ __forceinline__ float octet_sign(int octet, int cols) {
+  return (__popc(unsigned(octet & 15 & (cols / 8 - 1))) & 1) ? -1.f : 1.f;
+}
+
+// One such stage on eight registers. (As asm: from the builtin the compiler makes two moves and the
+// multiply-add. s_nop: a register read by DPP has to have been written two instructions before; each
+// of the eight was written by another of the same eight or before the s_nop.)
+#define KQ_DPP_STAGE(NAME, CTRL)                                                                  \
+  __device__ __forceinline__ void NAME(float* x, float s) {                                       \
+    asm("s_nop 1\n\t"                                                                             \
+        "v_fmac_f32_dpp %0, %0, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %1, %1, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %2, %2, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %3, %3, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %4, %4, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %5, %5, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %6, %6, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %7, %7, %8 " CTRL " row_mask:0xf bank_mask:0xf"                           \
+        : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]),     \
+          "+v"(x[7])                                                                              \
+        : "v"(s));                                                                                \
+  }
+KQ_DPP_STAGE(stage_lane1, "quad_perm:[1,0,3,2]")
+KQ_DPP_STAGE(stage_lane2, "quad_perm:[2,3,0,1]")
+KQ_DPP_STAGE(stage_mirror8, "row_half_mirror")
+KQ_DPP_STAGE(stage_lane8, "row_ror:8")
+#undef KQ_DPP_STAGE
+
+// (every lane of the wave comes here; FULL: columns of 512)
+template <int N, bool FULL>
+__device__ __forceinline__ void stages_dpp(float (&x)[8 * N], int octet, int cols) {
+  const float s0 = (octet & 1) ? -1.f : 1.f, s1 = (octet & 2) ? -1.f : 1.f;
+  const float s2 = (octet & 4) ? -1.f : 1.f, s3 = (octet & 8) ? -1.f : 1.f;
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    float v[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = x[8 * n + k];
-    hadamard_reg<8>(v);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[8 * n + k] = v[k];
+    float* v = x + 8 * n;
+    if (FULL || cols >= 128) {
+      stage_lane1(v, s0);
+      stage_lane2(v, s1);
+      stage_mirror8(v, s2);
+      stage_lane8(v, s3);
+    } else {
+      if (cols > 8) stage_lane1(v, s0);
+      if (cols > 16) stage_lane2(v, s1);
+      if (cols > 32) stage_mirror8(v, s2);
+    }
   }
-  if (cols >= 128) return hadamard_lanes<8 * N>(x, lane, cols == 128 ? 4 : cols == 256 ? 5 : 6);
-  const float s0 = (lane & 1) ? -1.f : 1.f, s1 = (lane & 2) ? -1.f : 1.f;
-  const float s2 = (lane & 4) ? -1.f : 1.f;
+}
+
+// registers k and k + 4 of each octet: sum and difference
+template <int N>
+__device__ __forceinline__ void stage_high(float (&x)[8 * N]) {
 #pragma unroll
-  for (int e = 0; e < 8 * N; ++e) {
-    if (cols > 8) x[e] = fmaf(x[e], s0, dpp_mov<0xB1>(x[e]));
-    if (cols > 16) x[e] = fmaf(x[e], s1, dpp_mov<0x4E>(x[e]));
-    if (cols > 32) x[e] = fmaf(x[e], s2, dpp_mov<0x1B>(dpp_mov<0x141>(x[e])));
+  for (int e = 0; e < 8 * N; ++e)
+    if (!(e & 4)) {
+      const float a = x[e], b = x[e + 4];
+      x[e] = a + b, x[e + 4] = a - b;
+    }
+}
+// exchange registers k + 4 of the lower 16 lanes (of each 32) or 32 lanes with registers k of the
+// upper: bit 2 of the register takes the place of lane bit 4 or 5, and that bit its place
+template <int N, bool WIDE>
+__device__ __forceinline__ void turn_high(float (&x)[8 * N]) {
+#pragma unroll
+  for (int e = 0; e < 8 * N; ++e)
+    if (!(e & 4)) {
+      const uint32_t a = __float_as_uint(x[e]), b = __float_as_uint(x[e + 4]);
+      if constexpr (WIDE) {
+        const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+        x[e] = __uint_as_float(r[0]), x[e + 4] = __uint_as_float(r[1]);
+      } else {
+        const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+        x[e] = __uint_as_float(r[0]), x[e + 4] = __uint_as_float(r[1]);
+      }
+    }
+}
+
+// The stages inside a column on octets of neighbours (octet_of the lane in each of N), up to
+// octet_sign. Elements 2^2, 2^7 and 2^8 apart are brought into one register bit, one after another.
+// What a lane holds at the start and at the end differs with columns of 512: register bit 2 and lane
+// bits 4 and 5 stand for element bits
+//   8-neighbours first:  (2, 7, 8) at the start, (8, 2, 7) at the end;
+//   8-neighbours last:   (7, 8, 2) at the start, (2, 7, 8) at the end.
+template <int N, bool FULL>
+__device__ __forceinline__ void inside_column(float (&x)[8 * N], int lane, int cols) {
+#pragma unroll
+  for (int e = 0; e < 8 * N; e += 4) {
+    float v[4] = {x[e], x[e + 1], x[e + 2], x[e + 3]};
+    hadamard_reg<4>(v);
+    x[e] = v[0], x[e + 1] = v[1], x[e + 2] = v[2], x[e + 3] = v[3];
   }
+  stages_dpp<N, FULL>(x, octet_of(lane), cols);
+  stage_high<N>(x);
+  if (!FULL && cols < 256) return;
+  turn_high<N, false>(x);
+  stage_high<N>(x);
+  if constexpr (FULL) {
+    turn_high<N, true>(x);
+    stage_high<N>(x);
+  } else {
+    turn_high<N, false>(x);  // (back)
+  }
+}
+// first element of registers 4 h to 4 h + 3 of a lane before (first) or after inside_column, among
+// the 512 of a wave
+template <bool FIRST, bool FULL>
+__device__ __forceinline__ int quad_at(int lane, int h) {
+  const int o = octet_of(lane), b4 = (lane >> 4) & 1, b5 = lane >> 5;
+  if (!FULL) return 8 * o + 4 * h;
+  return FIRST ? 8 * ((o & 15) | h << 4 | b4 << 5) + 4 * b5
+               : 8 * ((o & 15) | b5 << 4 | h << 5) + 4 * b4;
 }
 
 // Columns c = B a + b: H_B over b, and the 28 x 28 factor over a where C is 28 B (Q in LDS, row a
@@ -194,14 +289,14 @@ __device__ __forceinline__ void load8(const float* p, float* v) {
   }
 }
 
-// C: columns of a rotated row (0: not rotated). N: octets a thread ends with.
-template <typename T, int C, int N>
+// C: columns of a rotated row (0: not rotated), of 512 elements with FULL. N: octets a thread ends with.
+template <typename T, int C, int N, bool FULL>
 __global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, int lead) {
   extern __shared__ __attribute__((aligned(16))) float buf[];  // the row, when rotated
   __shared__ __attribute__((aligned(16))) float Q[C % 28 == 0 && C ? 784 : 4];
   __shared__ float red[4];
   __shared__ int sh[256];
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (int(blockIdx.x) < lead) {
     if (int(blockIdx.x) < table_blocks) fill_table(A, blockIdx.x);
     if (int(blockIdx.x) == lead - 1 && A.offsets) list_tiles(A, sh);
@@ -228,8 +323,8 @@ __global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, i
       for (int i = tid; i < 784; i += 256) Q[i] = q[i];
       __syncthreads();
     }
-    const int p = 2 * tid;
-    if (p < cols) {
+    const unsigned p = 2 * tid;
+    if (int(p) < cols) {
       float u[C], w[C];
 #pragma unroll
       for (int c = 0; c < C; ++c) load2(x + c * cols + p, u[c], w[c]);
@@ -246,18 +341,20 @@ __global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, i
     }
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int j = 8 * (tid + 256 * n);
-      float o[8] = {};
-      if (j < d) load8(buf + j, o);
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[8 * n + k] = o[k];
-    }
-    inside_column<N>(v, lane, cols);
+      for (int h = 0; h < 2; ++h) {
+        const int j = 512 * (wave + 4 * n) + quad_at<true, FULL>(lane, h);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (j < d) o = *reinterpret_cast<const float4*>(buf + j);
+        v[8 * n + 4 * h] = o.x, v[8 * n + 4 * h + 1] = o.y;
+        v[8 * n + 4 * h + 2] = o.z, v[8 * n + 4 * h + 3] = o.w;
+      }
+    inside_column<N, FULL>(v, lane, cols);
   } else {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int j = 8 * (tid + 256 * n);
+      const int j = 8 * (64 * (wave + 4 * n) + octet_of(lane));
       float o[8] = {};
       if (j < d) {
         load8(x + j, o);
@@ -278,16 +375,18 @@ __global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, i
   for (int k = 0; k < 8 * N; ++k) mx = fmaxf(mx, fabsf(v[k]));
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-  if (lane == 0) red[tid >> 6] = mx;
+  if (lane == 0) red[wave] = mx;
   __syncthreads();
   mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])) * A.turn.norm;
   const int e = int(__float_as_uint(mx) >> 23) - 127;
   const int ue = mx > 0.f && e < 128 ? clampi(e - 7, -100, 100) : 0;
-  const float up = pow2f(-ue) * A.turn.norm;
+  float up = pow2f(-ue) * A.turn.norm;
   if (tid == 0) A.row_unit[row] = pow2f(ue);
+  const int octet = octet_of(lane);
+  if constexpr (C > 0) up *= octet_sign(octet, A.turn.cols);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const int j = 8 * (tid + 256 * n);
+    const int j = 8 * (64 * (wave + 4 * n) + octet);
     float o[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -298,7 +397,7 @@ __global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, i
     // 2 bits a step takes four columns of either of two octets, which lie in neighbouring lanes
     float t[8];
     if (A.bits == 2) {
-      const bool odd = lane & 1;
+      const bool odd = octet & 1;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float got = dpp_mov<0xB1>(odd ? o[k] : o[4 + k]);
@@ -313,13 +412,18 @@ __global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, i
       for (int k = 0; k < 4; ++k) t[2 * k] = o[k], t[2 * k + 1] = o[4 + k];
     }
     if (j >= d) continue;
-    f16x8_t hi, lo;
+    f16x8_t hi;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) hi[k] = _Float16(t[k]), lo[k] = _Float16(t[k] - float(hi[k]));
+    for (int k = 0; k < 8; ++k) hi[k] = _Float16(t[k]);
     const int ks = (j >> 7) * 8 + ((j >> 5) & 1) * 4 + ((j >> 3) & 3), h = (j >> 6) & 1;
     uint16_t* to = A.xf + (((row >> 5) * (d / 16) + ks) * 64 + (row & 31) + 32 * h) * 8;
     *reinterpret_cast<f16x8_t*>(to) = hi;
-    if (A.planes == 2) *reinterpret_cast<f16x8_t*>(to + A.plane) = lo;
+    if (A.planes == 2) {
+      f16x8_t lo;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) lo[k] = _Float16(t[k] - float(hi[k]));
+      *reinterpret_cast<f16x8_t*>(to + A.plane) = lo;
+    }
   }
 }
 
@@ -350,14 +454,15 @@ __device__ __forceinline__ void store1(void* p, int64_t i, float v) {
     static_cast<float*>(p)[i] = v;
 }
 
-// bias, activation and residual of element j of a row
+// multiplier, bias, activation and residual of element j of a row (mul, bias and residual are the
+// row's, or null)
 template <typename T>
-__device__ __forceinline__ float finish(const LinearOut& A, int64_t row, int expert, int j, float v) {
-  const int64_t at = int64_t(expert) * A.d_out + j;
-  if (A.mul) v *= A.mul[at];
-  if (A.bias) v += A.bias[at];
-  v = activate(v, A.act);
-  if (A.residual) v += load1<T>(A.residual, row * A.ldr + j);
+__device__ __forceinline__ float finish(float v, unsigned j, const float* mul, const float* bias,
+                                        const T* residual, int act) {
+  if (mul) v *= mul[j];
+  if (bias) v += bias[j];
+  v = activate(v, act);
+  if (residual) v += load1<T>(residual, j);
   return v;
 }
 
@@ -446,12 +551,13 @@ struct Products {
 };
 
 // C columns of a rotated row of whole octets
-template <typename TP, typename T, int C>
+template <typename TP, typename T, int C, bool FULL>
 __global__ __launch_bounds__(256) void linear_out(LinearOut A) {
   extern __shared__ __attribute__((aligned(16))) float buf[];  // the row
   __shared__ __attribute__((aligned(16))) float Q[C % 28 == 0 ? 784 : 4];
   constexpr int N = C >= 4 ? C / 4 : 1;
-  const int tid = threadIdx.x, lane = tid & 63, d = int(A.d_out), cols = A.turn.cols;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int d = int(A.d_out), cols = A.turn.cols;
   const int64_t row = blockIdx.x;
   int expert = 0;
   if (A.offsets) {
@@ -465,31 +571,50 @@ __global__ __launch_bounds__(256) void linear_out(LinearOut A) {
   const Products<TP> products(A, row, expert);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const int j = 8 * (tid + 256 * n);
+    const int at = 512 * (wave + 4 * n), j = at + 8 * octet_of(lane);
     float v[8] = {};
     if (j < d) products.sum8(j, v);
-    inside_column<1>(v, lane, cols);
-    if (j < d) {
-      *reinterpret_cast<float4*>(buf + j) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(buf + j + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    inside_column<1, FULL>(v, lane, cols);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int q = at + quad_at<false, FULL>(lane, h);
+      if (q < d)
+        *reinterpret_cast<float4*>(buf + q) =
+            make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
     }
   }
   __syncthreads();
-  const int p = 2 * tid;
-  if (p >= cols) return;
-  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
+  const unsigned p = 2 * tid;
+  if (int(p) >= cols) return;
+  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit *
+                   octet_sign(int(p >> 3), cols);
   float u[C], w[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const float2 f = *reinterpret_cast<const float2*>(buf + c * cols + p);
     u[c] = f.x, w[c] = f.y;
   }
+  const float* const mul = A.mul ? A.mul + int64_t(expert) * d : nullptr;
+  const float* const bias = A.bias ? A.bias + int64_t(expert) * d : nullptr;
+  const T* const res = A.residual ? static_cast<const T*>(A.residual) + row * A.ldr : nullptr;
+  T* const y = static_cast<T*>(A.y) + row * A.ldy;
   across_columns<C>(u, w, Q, [&](int c, float a, float b) {
-    const int j = c * cols + p;
-    a = finish<T>(A, row, expert, j, a * up);
-    b = finish<T>(A, row, expert, j + 1, b * up);
-    store1<T>(A.y, row * A.ldy + j, a);
-    store1<T>(A.y, row * A.ldy + j + 1, b);
+    const unsigned j = c * cols + p;
+    a *= up, b *= up;
+    if (!A.pairs) {
+      store1<T>(y, j, finish<T>(a, j, mul, bias, res, A.act));
+      store1<T>(y, j + 1, finish<T>(b, j + 1, mul, bias, res, A.act));
+      return;
+    }
+    float f, g;
+    if (mul) load2(mul + j, f, g), a *= f, b *= g;
+    if (bias) load2(bias + j, f, g), a += f, b += g;
+    if (A.act != KRONQ_ACT_NONE) a = activate(a, A.act), b = activate(b, A.act);
+    if (res) load2(res + j, f, g), a += f, b += g;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint32_t*>(y + j) = uint32_t(f32_bf16(a)) | uint32_t(f32_bf16(b)) << 16;
+    else
+      *reinterpret_cast<float2*>(y + j) = make_float2(a, b);
   });
 }
 
@@ -506,13 +631,17 @@ __global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
     if (expert < 0) return;
   }
   const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
+  const float* const mul = A.mul ? A.mul + int64_t(expert) * d : nullptr;
+  const float* const bias = A.bias ? A.bias + int64_t(expert) * d : nullptr;
+  const T* const res = A.residual ? static_cast<const T*>(A.residual) + row * A.ldr : nullptr;
+  T* const y = static_cast<T*>(A.y) + row * A.ldy;
   const Products<TP> products(A, row, expert);
   for (int j = tid; j < d; j += 256) {
     const float v = products.sum1(j);
     if (A.turn.rotate)
       small[j] = v;  // (d <= 28 * 4)
     else
-      store1<T>(A.y, row * A.ldy + j, finish<T>(A, row, expert, j, v * up));
+      store1<T>(y, j, finish<T>(v * up, j, mul, bias, res, A.act));
   }
   if (!A.turn.rotate) return;
   __syncthreads();
@@ -524,7 +653,7 @@ __global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
       const float h = (__popc(unsigned(b & (k % A.turn.m))) & 1) ? -small[k] : small[k];
       v = fmaf(A.turn.has28 ? q[(k / A.turn.m) * 28 + a] : 1.f, h, v);
     }
-    store1<T>(A.y, row * A.ldy + j, finish<T>(A, row, expert, j, v * up));
+    store1<T>(y, j, finish<T>(v * up, j, mul, bias, res, A.act));
   }
 }
 
@@ -533,63 +662,69 @@ int in_typed(const LinearIn& a, hipStream_t s) {
   const int64_t table_blocks = a.table ? cdiv(a.w_rows, 8) : 0;
   const int64_t lead = cdiv(table_blocks + (a.offsets ? 1 : 0), 8) * 8;
   const dim3 grid(static_cast<unsigned>(lead + cdiv(a.n_rows, 256) * 256));
-#define KQ_IN(C_, N_)                                                                              \
-  launch("linear_in", linear_in<T, C_, N_>, grid, dim3(256), C_ ? size_t(a.d_in) * 4 : 0, s, a, \
+#define KQ_IN(C_, N_, F_)                                                                            \
+  launch("linear_in", linear_in<T, C_, N_, F_>, grid, dim3(256), C_ ? size_t(a.d_in) * 4 : 0, s, a, \
          int(table_blocks), int(lead))
   if (!a.turn.rotate) {
     const int64_t n = cdiv(a.d_in, 2048);
-    return n <= 1 ? KQ_IN(0, 1) : n <= 2 ? KQ_IN(0, 2) : n <= 4 ? KQ_IN(0, 4) : n <= 8 ? KQ_IN(0, 8)
-                                                                                  : KQ_IN(0, 16);
+    return n <= 1 ? KQ_IN(0, 1, false) : n <= 2 ? KQ_IN(0, 2, false) : n <= 4 ? KQ_IN(0, 4, false) : n <= 8 ? KQ_IN(0, 8, false)
+                                                                                  : KQ_IN(0, 16, false);
   }
+  const bool full = a.turn.cols == 512;
   switch (a.d_in / a.turn.cols) {
     case 1:
-      return KQ_IN(1, 1);
+      return full ? KQ_IN(1, 1, true) : KQ_IN(1, 1, false);
     case 2:
-      return KQ_IN(2, 1);
+      return KQ_IN(2, 1, true);
     case 4:
-      return KQ_IN(4, 1);
+      return KQ_IN(4, 1, true);
     case 8:
-      return KQ_IN(8, 2);
+      return KQ_IN(8, 2, true);
     case 16:
-      return KQ_IN(16, 4);
+      return KQ_IN(16, 4, true);
     case 32:
-      return KQ_IN(32, 8);
+      return KQ_IN(32, 8, true);
     case 64:
-      return KQ_IN(64, 16);
+      return KQ_IN(64, 16, true);
     case 28:
-      return KQ_IN(28, 7);
+      return full ? KQ_IN(28, 7, true) : KQ_IN(28, 7, false);
     default:
-      return KQ_IN(56, 14);
+      return KQ_IN(56, 14, true);
   }
 #undef KQ_IN
 }
 
 template <typename TP, typename T>
-int out_typed(const LinearOut& a, hipStream_t s) {
+int out_typed(LinearOut a, hipStream_t s) {
+  // two neighbours at once where every row of each operand begins on two
+  const size_t pair = 2 * sizeof(T);
+  a.pairs = aligned(a.y, pair) && a.ldy % 2 == 0 && aligned(a.bias, 8) &&
+            (!a.residual || (aligned(a.residual, pair) && a.ldr % 2 == 0));
   const dim3 grid(static_cast<unsigned>(a.n_rows));
   if (!a.turn.rotate || a.turn.cols < 8)
     return launch("linear_out", linear_out_any<TP, T>, grid, dim3(256), 0, s, a);
-#define KQ_OUT(C_) \
-  launch("linear_out", linear_out<TP, T, C_>, grid, dim3(256), size_t(a.d_out) * 4, s, a)
+#define KQ_OUT(C_, F_) \
+  launch("linear_out", linear_out<TP, T, C_, F_>, grid, dim3(256), size_t(a.d_out) * 4, s, a)
+  const bool full = a.turn.cols == 512;
   switch (a.d_out / a.turn.cols) {
     case 1:
-      return KQ_OUT(1);
+      return full ? KQ_OUT(1, true) : KQ_OUT(1, false);
     case 2:
-      return KQ_OUT(2);
+      return KQ_OUT(2, true);
     case 4:
-      return KQ_OUT(4);
+      return KQ_OUT(4, true);
     case 8:
-      return KQ_OUT(8);
+      return KQ_OUT(8, true);
     case 16:
-      return KQ_OUT(16);
+      return KQ_OUT(16, true);
     case 32:
-      return KQ_OUT(32);
+      return KQ_OUT(32, true);
     case 64:
-      return KQ_OUT(64);
+      return KQ_OUT(64, true);
     case 28:
-      return KQ_OUT(28);
+      return full ? KQ_OUT(28, true) : KQ_OUT(28, false);
     default:
-      return KQ_OUT(56);
+      return KQ_OUT(56, true);
   }
 #undef KQ_OUT
 }
