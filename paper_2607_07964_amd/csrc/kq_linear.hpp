@@ -12,10 +12,11 @@ struct LinearTile {
   int expert, unit, lo, hi;
 };
 
-// Many rows: the outputs are cut into items of a row tile and 256 rows of W, tile after tile, which
+// The outputs are cut into items of a row tile and a block of rows of W, tile after tile, which
 // `workers` workgroups share: whole items in full rounds, and the groups of columns of the items left
-// over in equal parts, `per` groups a worker in item order. So the last round is as full as the others;
-// a worker that begins inside an item keeps that part in a place of its own, for linear_out to add.
+// over in equal parts, `per` groups a worker in item order. So the last round is as full as the others
+// and few items keep the whole chip busy, however the rows fall to experts; a worker that begins inside
+// an item keeps that part in a place of its own, for linear_out to add.
 struct LinearDeal {
   int full, per;  // rounds of whole items; groups of the rest per worker
 };
@@ -28,7 +29,6 @@ __host__ __device__ inline LinearDeal linear_deal(int items, int ng, int workers
   if (per * 10 > ng * 9) per = ng;
   return LinearDeal{full, per};
 }
-constexpr int LINEAR_BLOCK = 256;  // rows of W of an item
 
 // Column (of a chunk of 32) of element i of step jj of a lane's eight codes, in the order in which
 // the codes of a packed chunk are spread to pairs of fp16.
@@ -77,13 +77,11 @@ int linear_in_launch(const LinearIn& a, hipStream_t s);
 
 // y = act(diag(mul_out) T_out y' + bias) + residual
 struct LinearOut {
-  // y': the sum of the splits, fp32 [split][row][ld]; or dealt (workers > 0): [row][ld] and the parts
-  // that workers keep, [worker][32 nt][LINEAR_BLOCK], both fp16 to be multiplied by w_unit (with
-  // w_unit) or fp32
+  // y' [row][ld]; dealt (workers > 0), with the parts that workers keep, [worker][32 nt][block]. Both
+  // fp16 to be multiplied by w_unit (with w_unit) or fp32.
   const void* part;
-  int64_t ld, stride;
-  int splits;
-  int workers, ng, nt, row_blocks, items;  // items without offsets
+  int64_t ld;
+  int workers, ng, nt, block, row_blocks, items;  // items without offsets
   const void* kept;
   const float* w_unit;
   const LinearTile* tiles;

@@ -7,7 +7,7 @@
 //   1. linear_in: x' as fp16 in MFMA-fragment order, each row scaled by a power of two of its own
 //      that brings its largest value into [2^7, 2^8); beside it the tables of the weights' scales
 //      and zeros, and for experts the list of row tiles.
-//   2. linear_mfma: products of 32 rows and 32 rows of W_hat' on v_mfma_f32_32x32x16_f16. A lane
+//   2. linear_ring: products of 32 rows and 32 rows of W_hat' on v_mfma_f32_32x32x16_f16. A lane
 //      reads the packed codes of its own weight row and spreads them to fp16 in registers.
 //   3. linear_out: the transform of y', and the epilogue.
 // Weights enter the matrix products in one of two forms (SCALED below): as fp16 s (c - z), each row
@@ -56,10 +56,10 @@ struct MmArgs {
   int gpq;
   const Tile* tiles;  // null: one layer, unit tiles in order
   int64_t n_rows;
-  int row_blocks, splits, per;  // groups per split
-  void* part;         // linear_mfma: fp32 [split][row][ld]; linear_ring: [row][ld]
+  int row_blocks;
+  void* part;         // [row][ld]
   int64_t ld;
-  void* kept;         // linear_ring: [worker][32 NT][LINEAR_BLOCK]
+  void* kept;         // [worker][32 NT][rows of W of an item]
   float down;         // of fp16 results
 };
 
@@ -135,88 +135,9 @@ __device__ __forceinline__ u32x4_t spread_int(const uint32_t* w, int jj, uint32_
   }
 }
 
-// this lane's codes of a group: two chunks of 32
-template <int BITS>
-__device__ __forceinline__ void load_codes(uint32_t (&w)[2 * BITS], const uint32_t* p) {
-  if constexpr (BITS == 3) {
-#pragma unroll
-    for (int k = 0; k < 6; k += 2) {
-      const uint2 v = *reinterpret_cast<const uint2*>(p + k);
-      w[k] = v.x, w[k + 1] = v.y;
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 2 * BITS; k += 4) {
-      const uint4 v = *reinterpret_cast<const uint4*>(p + k);
-      w[k] = v.x, w[k + 1] = v.y, w[k + 2] = v.z, w[k + 3] = v.w;
-    }
-  }
-}
-
 __device__ __forceinline__ f32x16_t mfma(u32x4_t a, u32x4_t b, f32x16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a),
                                                 __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-}
-
-// Few rows. A workgroup of four waves takes 128 rows of W (32 a wave) and a tile of NT units of rows
-// of x'; a lane holds the codes of one row of W and half of the columns.
-template <int BITS, int NT, int PLANES>
-__global__ __launch_bounds__(256) void linear_mfma(MmArgs A) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int split = blockIdx.y;
-  const int rb = blockIdx.x % A.row_blocks, ti = blockIdx.x / A.row_blocks;
-  Tile t;
-  if (A.tiles) {
-    if (ti >= A.tiles[0].expert) return;
-    t = A.tiles[1 + ti];
-  } else {
-    t = Tile{0, ti * NT, 0, int(A.n_rows)};
-  }
-  const int g0 = split * A.per, g1 = g0 + A.per < A.ng ? g0 + A.per : A.ng;
-  const int64_t n = int64_t(rb) * 128 + wave * 32 + (lane & 31);
-  const int last = (t.hi - 1) >> 5;  // last unit
-  const uint16_t* xa[NT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i)
-    xa[i] = A.xf + (t.unit + i < last ? t.unit + i : last) * int64_t(A.ng) * 4096 + lane * 8;
-  const int64_t wr = int64_t(t.expert) * A.d_out + (n < A.d_out ? n : A.d_out - 1);
-  const uint32_t* wp = A.packed + wr * A.ldp + (lane >> 5) * 2 * BITS;
-  f32x16_t acc[NT] = {};
-  for (int g = g0; g < g1; ++g) {
-    uint32_t w[2 * BITS];
-    load_codes<BITS>(w, wp + int64_t(g) * 4 * BITS);
-    const int64_t at = wr * A.ldsz + unsigned(g) / unsigned(A.gpq);
-    const _Float16 nz = _Float16(-1024.f - A.zeros[at]);
-    const float sc = A.scales[at];
-    f32x16_t sum[NT] = {};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const u32x4_t b = spread_int<BITS>(w + (j >> 2) * BITS, j & 3, u2(f16x2_t{nz, nz}));
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        const uint16_t* p = xa[i] + (int64_t(g) * 8 + j) * 512;
-        const u32x4_t a = *reinterpret_cast<const u32x4_t*>(p);
-        if constexpr (PLANES == 2)
-          sum[i] = mfma(*reinterpret_cast<const u32x4_t*>(p + A.plane), b, sum[i]);
-        sum[i] = mfma(a, b, sum[i]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][r] = fmaf(sc, sum[i][r], acc[i][r]);
-  }
-  float* part = static_cast<float*>(A.part) + int64_t(split) * A.n_rows * A.ld;
-  if (n >= A.d_out) return;
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int64_t m0 = int64_t(t.unit + i) * 32 + 4 * (lane >> 5);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int64_t m = m0 + 8 * (r >> 2) + (r & 3);
-      if (m >= t.lo && m < t.hi) part[m * A.ld + n] = acc[i][r];
-    }
-  }
 }
 
 template <int N>
@@ -247,19 +168,26 @@ __device__ __forceinline__ Chunk<BITS> load_chunk(const uint32_t* p) {
   return c;
 }
 
-// Many rows. As above with x' through LDS: a stage is 64 columns (half a group, a chunk of each
-// lane's codes) of NT units in PLANES planes, NT PLANES = 4 pieces of 4 KB of which each wave brings
-// one straight to LDS, in fragment order as it stands, through a ring of four stages. One barrier a
-// stage, in its middle: it publishes the next stage and frees the buffer of the one before, which the
-// loads of three stages on then fill; operands are read one step of 16 columns ahead. Two workgroups
-// per CU (64 KB of LDS and 256 registers a lane each), so that one wave's spreading of codes runs
-// beside the other's matrix instructions. Scaled results leave as fp16 (linear_out multiplies by the
-// units of the rows of W).
-template <int BITS, int NT, int PLANES>
-__global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
-  constexpr int RT = 2, STAGE = 4 * 1024, R = 4;  // (dwords)
-  constexpr bool SCALED = PLANES == 1;
-  static_assert(NT * PLANES == 4, "one piece of a stage per wave");
+// A workgroup of four waves takes 128 RT rows of W (32 RT a wave) and a tile of NT units of rows of
+// x'; a lane holds the codes of RT rows of W and half of the columns, 64 of them a stage. x' comes
+// through LDS: a stage is 64 columns (half a group, a chunk of each lane's codes) of NT units in
+// PLANES planes, pieces of 4 KB that the waves bring straight to LDS, in fragment order as they
+// stand, through a ring of four stages. One barrier a stage, in its middle: it publishes the next
+// stage and frees the buffer of the one before, which the loads of three stages on then fill;
+// operands are read one step of 16 columns ahead.
+//   SCALED, NT = 4, RT = 2 (many rows): the matrix instructions bound it. Two workgroups per CU (64 KB
+//     of LDS and 256 registers a lane each), so that one wave's spreading of codes runs beside the
+//     other's matrix instructions. Results leave as fp16 (linear_out multiplies by the units of the
+//     rows of W).
+//   PLANES = 2, NT = 2, RT = 2: the same for fp32 results.
+//   RT = 1 (few rows): the codes' way from memory bounds it; four workgroups per CU keep the loads of
+//     16 waves out at a time.
+constexpr int per_cu(int rt) { return rt == 2 ? 2 : 4; }
+
+template <int BITS, int NT, int PLANES, int RT, bool SCALED>
+__global__ __launch_bounds__(256, per_cu(RT)) void linear_ring(MmArgs A) {
+  constexpr int NP = NT * PLANES, STAGE = NP * 1024, R = 4, BLOCK = 128 * RT;  // (STAGE: dwords)
+  static_assert(!SCALED || PLANES == 1, "fp32 results take exact weights");
   __shared__ __attribute__((aligned(16))) uint32_t lds[R * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Workers that share an XCD (workgroup % 8) stand next to one another in the deal, so that the x'
@@ -286,23 +214,24 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
     }
     const int rb = item % A.row_blocks, ti = item / A.row_blocks;
     const Tile t = A.tiles ? A.tiles[1 + ti] : Tile{0, ti * NT, 0, int(A.n_rows)};
-    const int64_t n0 = int64_t(rb) * (128 * RT) + wave * (32 * RT);
+    const int64_t n0 = int64_t(rb) * BLOCK + wave * (32 * RT);
     const int last = (t.hi - 1) >> 5;  // last unit
     const int nst = 2 * (g1 - g0);
-    const int un = t.unit + wave / PLANES;
+    // this wave's piece of a stage, and the first of the NP of its four steps that it brings
+    const int piece = wave % NP, step = wave / NP * NP, un = t.unit + piece / PLANES;
     // (buffer loads: beside global_load_lds the compiler waits for every outstanding load before it
     // uses one that went to a register)
-    const uint16_t* const piece = A.xf + (PLANES == 2 ? (wave & 1) * A.plane : 0) +
-                                  (un < last ? un : last) * int64_t(A.ng) * 4096;
-    const auto src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(piece), 0, A.ng * 8192,
+    const uint16_t* const rows = A.xf + (piece % PLANES) * A.plane +
+                                 (un < last ? un : last) * int64_t(A.ng) * 4096;
+    const auto src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(rows), 0, A.ng * 8192,
                                                        0x00027000);
     auto issue = [&](int st) {  // past the end: the last stage again, never read
       const int at = (2 * g0 + (st < nst ? st : nst - 1)) * 4096;
-      uint32_t* dst = lds + (st & (R - 1)) * STAGE + wave * 1024;
+      uint32_t* dst = lds + (st & (R - 1)) * STAGE + piece * 1024;
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, KQ_LDS(dst + q * 256), 16, lane * 16,
-                                                 at + q * 1024, 0, 0);
+      for (int q = 0; q < NP; ++q)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, KQ_LDS(dst + (step + q) * 256), 16, lane * 16,
+                                                 at + (step + q) * 1024, 0, 0);
     };
     const uint32_t* wp[RT];
     int64_t wr[RT];
@@ -340,11 +269,11 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int st = 0; st < 3; ++st) issue(st);
-    u32x4_t a[2][4];
+    u32x4_t a[2][NP];
     auto frags = [&](int st, int q) {
       const uint32_t* buf = lds + (st & (R - 1)) * STAGE + lane * 4 + q * 256;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[q & 1][i] = *reinterpret_cast<const u32x4_t*>(buf + i * 1024);
+      for (int i = 0; i < NP; ++i) a[q & 1][i] = *reinterpret_cast<const u32x4_t*>(buf + i * 1024);
     };
     uint32_t z[RT];
     auto stage = [&](int st, auto hc) {
@@ -365,9 +294,9 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         if (q == 2) {
-          // the next stage's loads have landed (those of the one after it may be out, and what this
-          // wave has requested of codes since)
-          wait_vm<8>();
+          // the next stage's loads have landed (the NP of the one after it may be out, and what this
+          // wave has requested of codes before and after those, RT loads at least each)
+          wait_vm<NP + 2 * RT>();
           __builtin_amdgcn_s_barrier();
           issue(st + 3);
           __builtin_amdgcn_sched_barrier(0);
@@ -384,8 +313,8 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
             if constexpr (SCALED) {
               acc[i][k] = mfma(a[q & 1][i], b[k], acc[i][k]);
             } else {
-              sum[i][k] = mfma(a[q & 1][2 * i + 1], b[k], sum[i][k]);
-              sum[i][k] = mfma(a[q & 1][2 * i], b[k], sum[i][k]);
+              if constexpr (PLANES == 2) sum[i][k] = mfma(a[q & 1][2 * i + 1], b[k], sum[i][k]);
+              sum[i][k] = mfma(a[q & 1][PLANES * i], b[k], sum[i][k]);
             }
           }
         __builtin_amdgcn_sched_barrier(0);  // (else every step's operands are read at once, and spill)
@@ -404,7 +333,7 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
         }
       }
     };
-    wait_vm<8>();
+    wait_vm<2 * NP>();
     __builtin_amdgcn_s_barrier();
     frags(0, 0);
     for (int st = 0; st < nst; st += 2) {
@@ -415,10 +344,9 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
     __builtin_amdgcn_s_barrier();
     // a worker that began inside an item keeps its part
     using Part = std::conditional_t<SCALED, _Float16, float>;
-    const int64_t ld = g0 > 0 ? LINEAR_BLOCK : A.ld;
+    const int64_t ld = g0 > 0 ? BLOCK : A.ld;
     Part* const part =
-        g0 > 0 ? static_cast<Part*>(A.kept) + (int64_t(id) * NT - t.unit) * 32 * LINEAR_BLOCK -
-                     rb * LINEAR_BLOCK
+        g0 > 0 ? static_cast<Part*>(A.kept) + (int64_t(id) * NT - t.unit) * 32 * BLOCK - rb * BLOCK
                : static_cast<Part*>(A.part);
 #pragma unroll
     for (int k = 0; k < RT; ++k) {
@@ -448,8 +376,8 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
 constexpr int64_t GEMV_ROWS = 4, GEMV_INPUTS = 32768;
 
 struct Plan {
-  int planes, nt, splits, per, workers;
-  bool ring, scaled;
+  int planes, nt, rt, workers, block;
+  bool scaled;
   float down;
   int64_t tiles, row_blocks;
 };
@@ -457,25 +385,19 @@ struct Plan {
 Plan make_plan(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts, int y_dtype) {
   Plan p;
   p.planes = y_dtype == KRONQ_BF16 ? 1 : 2;
-  const int64_t per_expert = cdiv(n_rows, n_experts), ng = d_in / 128;
-  p.ring = per_expert > 64;
-  p.scaled = p.ring && p.planes == 1;
-  p.nt = p.ring ? 4 / p.planes : per_expert > 32 ? 2 : 1;
+  // A tile of 32 rows for up to 32 rows (of an expert), of 64 up to 64; more rows share the spread
+  // codes best in tiles of 128 (64 in two planes).
+  const int64_t rows = cdiv(n_rows, n_experts);
+  p.scaled = p.planes == 1 && rows > 64;
+  p.nt = p.scaled ? 4 : rows > 32 ? 2 : 1;
+  p.rt = p.nt * p.planes == 4 ? 2 : 1;
+  p.block = 128 * p.rt;
   p.tiles = n_experts == 1 ? cdiv(n_rows, 32 * p.nt) : most_tiles(n_rows, n_experts, p.nt);
-  p.row_blocks = cdiv(d_out, p.ring ? LINEAR_BLOCK : 128);
-  p.splits = 1, p.per = int(ng), p.workers = 0, p.down = 1.f;
-  if (p.ring) {
-    p.workers = device_cus() / 4 * 8;  // two per CU
-    // fp16 results: below 2^8 (x') times 2.5 (|c - z| < 1280 of at most 2^-9) times d_in
-    while (p.scaled && 640.f * float(d_in) * p.down > 65000.f) p.down *= 0.5f;
-    return p;
-  }
-  const int64_t wgs = p.tiles * p.row_blocks;
-  int64_t s = wgs < 512 ? 512 / wgs : 1;
-  if (s > ng) s = ng;
-  if (s > 16) s = 16;
-  p.per = int(cdiv(ng, s));
-  p.splits = int(cdiv(ng, p.per));
+  p.row_blocks = cdiv(d_out, p.block);
+  p.workers = device_cus() / 8 * 8 * per_cu(p.rt);
+  // fp16 results: below 2^8 (x') times 2.5 (|c - z| < 1280 of at most 2^-9) times d_in
+  p.down = 1.f;
+  while (p.scaled && 640.f * float(d_in) * p.down > 65000.f) p.down *= 0.5f;
   return p;
 }
 
@@ -496,8 +418,8 @@ Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, i
   w.xf = cv.take<uint16_t>(size_t(p.planes) * size_t(cdiv(n_rows, 32) * 32) * size_t(d_in));
   w.row_unit = cv.take<float>(size_t(n_rows));
   const size_t size = p.scaled ? 2 : 4;  // of a product
-  w.part = cv.take<char>(size_t(p.splits) * size_t(n_rows) * size_t(cdiv(d_out, 8) * 8) * size);
-  w.kept = cv.take<char>(size_t(p.workers) * size_t(32 * p.nt) * LINEAR_BLOCK * size);
+  w.part = cv.take<char>(size_t(n_rows) * size_t(cdiv(d_out, 8) * 8) * size);
+  w.kept = cv.take<char>(size_t(p.workers) * size_t(32 * p.nt) * size_t(p.block) * size);
   const size_t w_rows = p.scaled ? size_t(n_experts) * size_t(d_out) : 0;
   w.w_unit = cv.take<float>(w_rows);
   w.table = cv.take<uint32_t>(w_rows * size_t(d_in / 128));
@@ -509,17 +431,12 @@ Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, i
 
 template <int BITS>
 int launch_mm(const MmArgs& a, const Plan& p, hipStream_t s) {
-  if (p.ring) {
-    const dim3 grid(static_cast<unsigned>(p.workers));
-    return p.planes == 1
-               ? launch("linear_ring", linear_ring<BITS, 4, 1>, grid, dim3(256), 0, s, a)
-               : launch("linear_ring", linear_ring<BITS, 2, 2>, grid, dim3(256), 0, s, a);
-  }
-  const dim3 grid(static_cast<unsigned>(p.tiles * p.row_blocks), static_cast<unsigned>(p.splits));
-#define KQ_MM(NT_, PL_) \
-  launch("linear_mfma", linear_mfma<BITS, NT_, PL_>, grid, dim3(256), 0, s, a)
-  if (p.planes == 1) return p.nt == 1 ? KQ_MM(1, 1) : KQ_MM(2, 1);
-  return p.nt == 1 ? KQ_MM(1, 2) : KQ_MM(2, 2);
+  const dim3 grid(static_cast<unsigned>(p.workers));
+#define KQ_MM(NT_, PL_, RT_, SC_) \
+  launch("linear_ring", linear_ring<BITS, NT_, PL_, RT_, SC_>, grid, dim3(256), 0, s, a)
+  if (p.scaled) return KQ_MM(4, 1, 2, true);
+  if (p.planes == 1) return p.nt == 1 ? KQ_MM(1, 1, 1, false) : KQ_MM(2, 1, 1, false);
+  return p.nt == 1 ? KQ_MM(1, 2, 1, false) : KQ_MM(2, 2, 2, false);
 #undef KQ_MM
 }
 
@@ -548,7 +465,7 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
     KQ_TRY(online_product_launch(j.packed, j.ldp, j.scales, j.zeros, j.ldsz, j.bits, j.group,
                                  j.d_out, j.d_in, j.mul_in, j.q28_in, j.flags, j.x, j.x_dtype,
                                  j.ldx, j.n_rows, ws, &yr, s));
-    o.part = yr, o.ld = j.d_out, o.splits = 1, o.unit = 1.f;
+    o.part = yr, o.ld = j.d_out, o.unit = 1.f;
     return linear_out_launch(o, s);
   }
   const Plan p = make_plan(j.d_out, j.d_in, j.n_rows, j.n_experts, j.y_dtype);
@@ -569,13 +486,13 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
   m.xf = w.xf, m.plane = a.plane, m.ng = a.ng, m.table = w.table, m.w_unit = w.w_unit;
   m.scales = j.scales, m.zeros = j.zeros, m.ldsz = j.ldsz, m.gpq = a.gpq;
   m.tiles = j.offsets ? w.tiles : nullptr, m.n_rows = j.n_rows;
-  m.row_blocks = int(p.row_blocks), m.splits = p.splits, m.per = p.per;
+  m.row_blocks = int(p.row_blocks);
   m.part = w.part, m.ld = cdiv(j.d_out, 8) * 8, m.kept = w.kept, m.down = p.down;
   KQ_TRY(j.bits == 2   ? launch_mm<2>(m, p, s)
          : j.bits == 3 ? launch_mm<3>(m, p, s)
          : j.bits == 4 ? launch_mm<4>(m, p, s)
                        : launch_mm<8>(m, p, s));
-  o.part = w.part, o.ld = m.ld, o.stride = j.n_rows * m.ld, o.splits = p.splits;
+  o.part = w.part, o.ld = m.ld, o.block = p.block;
   o.row_unit = w.row_unit, o.unit = 1.f / p.down;
   o.workers = p.workers, o.ng = a.ng, o.nt = p.nt, o.row_blocks = m.row_blocks, o.kept = w.kept;
   o.items = int(p.tiles * p.row_blocks), o.w_unit = p.scaled ? w.w_unit : nullptr;

@@ -5,7 +5,7 @@
 // 256 threads takes a row, as d / cols columns of cols = min(m, 512) elements. Its two factors touch
 // the row in two ways that meet once in LDS:
 //   across the columns (A and the upper stages of H): a thread holds the same two elements of every
-//     column, 2 d / cols registers, and mixes them in place;
+//     column, 2 d / cols registers, and mixes them in place (A = Q28: mix28);
 //   inside a column (the lower nine stages of H): a lane holds 8 neighbours, three stages in
 //     registers, six across lanes by DPP.
 // The input side goes across first, straight from the row in memory, and ends with 8 neighbours per
@@ -35,22 +35,22 @@ __device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? l
 // workgroup calls it.
 __device__ __forceinline__ int expert_of(const int* offsets, int n_experts, int64_t row) {
   int n = 0;  // experts whose range ends at or before the row
-  for (int e0 = 0; e0 < n_experts; e0 += 256) {
+  for (int e0 = 0; e0 < n_experts; e0 += int(blockDim.x)) {
     const int e = e0 + int(threadIdx.x);
     n += __syncthreads_count(e < n_experts && offsets[e + 1] <= row);
   }
   return n >= n_experts || row < offsets[0] ? -1 : n;
 }
 
-// The list of tiles, by one workgroup of 256 threads: the experts' ranges made ascending and cut to
+// The list of tiles, by one workgroup: the experts' ranges made ascending and cut to
 // [0, n_rows), so that no content of offsets leads out of the rows.
 __device__ void list_tiles(const LinearIn& A, int* sh) {
-  const int tid = threadIdx.x, n = int(A.n_rows);
+  const int tid = threadIdx.x, thr = blockDim.x, n = int(A.n_rows);
   int base = 0, top = clampi(A.offsets[0], 0, n);  // tiles so far, largest offset so far
-  for (int e0 = 0; e0 < A.n_experts; e0 += 256) {
+  for (int e0 = 0; e0 < A.n_experts; e0 += thr) {
     const int e = e0 + tid;
     int v = e < A.n_experts ? clampi(A.offsets[e + 1], 0, n) : 0;
-    for (int o = 1; o < 256; o <<= 1) {  // running maximum over the threads
+    for (int o = 1; o < thr; o <<= 1) {  // running maximum over the threads
       sh[tid] = v;
       __syncthreads();
       if (tid >= o) v = max(v, sh[tid - o]);
@@ -60,12 +60,12 @@ __device__ void list_tiles(const LinearIn& A, int* sh) {
     sh[tid] = v;
     __syncthreads();
     const int lo = tid ? sh[tid - 1] : top, hi = v;
-    top = sh[255];
+    top = sh[thr - 1];
     __syncthreads();
     const int u0 = lo >> 5, nu = hi > lo ? ((hi - 1) >> 5) - u0 + 1 : 0;
     const int k = (nu + A.nt - 1) / A.nt;
     int sum = k;  // (running over the threads)
-    for (int o = 1; o < 256; o <<= 1) {
+    for (int o = 1; o < thr; o <<= 1) {
       sh[tid] = sum;
       __syncthreads();
       if (tid >= o) sum += sh[tid - o];
@@ -78,15 +78,15 @@ __device__ void list_tiles(const LinearIn& A, int* sh) {
     }
     sh[tid] = sum;
     __syncthreads();
-    base += sh[255];
+    base += sh[thr - 1];
     __syncthreads();
   }
   if (tid == 0) A.tiles[0] = LinearTile{base < A.max_tiles ? base : int(A.max_tiles), 0, 0, 0};
 }
 
-// the table of eight rows of W: 32 threads take a row
+// the table of a workgroup's rows of W: 32 threads take a row
 __device__ void fill_table(const LinearIn& A, int64_t block) {
-  const int64_t row = block * 8 + (threadIdx.x >> 5);
+  const int64_t row = block * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int t = threadIdx.x & 31;
   if (row >= A.w_rows) return;
   const float *s = A.scales + row * A.ldsz, *z = A.zeros + row * A.ldsz;
@@ -226,42 +226,51 @@ __device__ __forceinline__ int quad_at(int lane, int h) {
                : 8 * ((o & 15) | b5 << 4 | h << 5) + 4 * b4;
 }
 
-// Columns c = B a + b: H_B over b, and the 28 x 28 factor over a where C is 28 B (Q in LDS, row a
-// holding the factors of output a). put(c, x, y) takes the results of both elements.
+// H_C over the columns of two elements: put(c, x, y) takes the results.
 template <int C, typename Put>
-__device__ __forceinline__ void across_columns(float (&x)[C], float (&y)[C], const float* Q,
-                                               Put put) {
-  if constexpr (C % 28 != 0) {
-    hadamard_reg<C>(x);
-    hadamard_reg<C>(y);
+__device__ __forceinline__ void across_columns(float (&x)[C], float (&y)[C], Put put) {
+  hadamard_reg<C>(x);
+  hadamard_reg<C>(y);
 #pragma unroll
-    for (int c = 0; c < C; ++c) put(c, x[c], y[c]);
-  } else {
-    constexpr int B = C / 28;
-    if constexpr (B == 2) {
+  for (int c = 0; c < C; ++c) put(c, x[c], y[c]);
+}
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+// The 28 x 28 factor over the segments of m elements of the row in LDS, on the fp32 matrix cores (as
+// multiply-adds of a thread's own elements it took three times as long: two chains of 28 at a time),
+// and, for m = 1024 (B = 2), the stage of stride 512 that a column of 512 leaves out. A wave takes
+// 32 places of every segment at a time; place(i, v): element i of the row has become v.
+template <int B, bool TRANS, typename Place>
+__device__ __forceinline__ void mix28(const float* buf, int m, const float* __restrict__ q28,
+                                      int wave, int waves, int lane, Place place) {
+  const int n = lane & 31, half = lane >> 5;
+  float q[14];
 #pragma unroll
-      for (int c = 0; c < C; c += 2) {
-        const float a = x[c], b = x[c + 1], d = y[c], e = y[c + 1];
-        x[c] = a + b, x[c + 1] = a - b, y[c] = d + e, y[c + 1] = d - e;
+  for (int s = 0; s < 14; ++s) {
+    const int k = 2 * s + half, a = n < 28 ? n : 27;
+    q[s] = q28[TRANS ? k * 28 + a : a * 28 + k];  // (rows 28 to 31 are not used)
+  }
+  const int cols = B == 2 ? 512 : m;
+  for (int p0 = 32 * wave; p0 < cols; p0 += 32 * waves) {
+    const int p = p0 + n, pc = p < cols ? p : cols - 1;
+    f32x16_t d[B] = {};
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int s = 0; s < 14; ++s)
+        d[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(q[s], buf[(2 * s + half) * m + 512 * b + pc],
+                                                    d[b], 0, 0, 0);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int a = 8 * (r >> 2) + 4 * half + (r & 3);
+      if (a >= 28 || p >= cols) continue;
+      if constexpr (B == 2) {
+        place(a * m + p, d[0][r] + d[1][r]);
+        place(a * m + p + 512, d[0][r] - d[1][r]);
+      } else {
+        place(a * m + p, d[0][r]);
       }
-    }
-#pragma unroll 2
-    for (int a = 0; a < 28; ++a) {
-      float u[B] = {}, v[B] = {};
-#pragma unroll
-      for (int k = 0; k < 28; k += 4) {
-        const float4 q = *reinterpret_cast<const float4*>(Q + a * 28 + k);
-        const float f[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int b = 0; b < B; ++b) {
-            u[b] = fmaf(f[i], x[(k + i) * B + b], u[b]);
-            v[b] = fmaf(f[i], y[(k + i) * B + b], v[b]);
-          }
-      }
-#pragma unroll
-      for (int b = 0; b < B; ++b) put(a * B + b, u[b], v[b]);
     }
   }
 }
@@ -289,13 +298,16 @@ __device__ __forceinline__ void load8(const float* p, float* v) {
   }
 }
 
+// Threads of a workgroup. A row of 28 m takes most of the LDS of half a CU: 16 waves hide its steps.
+constexpr int threads(int c) { return c && c % 28 == 0 ? 1024 : 256; }
+
 // C: columns of a rotated row (0: not rotated), of 512 elements with FULL. N: octets a thread ends with.
 template <typename T, int C, int N, bool FULL>
-__global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, int lead) {
+__global__ __launch_bounds__(threads(C)) void linear_in(LinearIn A, int table_blocks, int lead) {
   extern __shared__ __attribute__((aligned(16))) float buf[];  // the row, when rotated
-  __shared__ __attribute__((aligned(16))) float Q[C % 28 == 0 && C ? 784 : 4];
-  __shared__ float red[4];
-  __shared__ int sh[256];
+  constexpr int THR = threads(C), WAVES = THR / 64;
+  __shared__ float red[WAVES];
+  __shared__ int sh[THR];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (int(blockIdx.x) < lead) {
     if (int(blockIdx.x) < table_blocks) fill_table(A, blockIdx.x);
@@ -319,32 +331,49 @@ __global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, i
   if constexpr (C > 0) {
     const int cols = A.turn.cols;
     if constexpr (C % 28 == 0) {
-      const float* q = A.q28 + int64_t(expert) * 784;
-      for (int i = tid; i < 784; i += 256) Q[i] = q[i];
-      __syncthreads();
-    }
-    const unsigned p = 2 * tid;
-    if (int(p) < cols) {
-      float u[C], w[C];
 #pragma unroll
-      for (int c = 0; c < C; ++c) load2(x + c * cols + p, u[c], w[c]);
-      if (mul) {
+      for (int n = 0; n < N; ++n) {
+        const int j = 8 * (tid + THR * n);
+        if (j >= d) continue;
+        float o[8];
+        load8(x + j, o);
+        if (mul) {
+          float f[8];
+          load8(mul + j, f);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const float2 f = *reinterpret_cast<const float2*>(mul + c * cols + p);
-          u[c] *= f.x, w[c] *= f.y;
+          for (int k = 0; k < 8; ++k) o[k] *= f[k];
         }
+        *reinterpret_cast<float4*>(buf + j) = make_float4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<float4*>(buf + j + 4) = make_float4(o[4], o[5], o[6], o[7]);
       }
-      across_columns<C>(u, w, Q, [&](int c, float a, float b) {
-        *reinterpret_cast<float2*>(buf + c * cols + p) = make_float2(a, b);
-      });
+      __syncthreads();
+      // (in place: a wave reads all of its 32 places before it writes them)
+      mix28<C / 28, false>(buf, A.turn.m, A.q28 + int64_t(expert) * 784, wave, WAVES, lane,
+                           [&](int i, float v) { buf[i] = v; });
+    } else {
+      const unsigned p = 2 * tid;
+      if (int(p) < cols) {
+        float u[C], w[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) load2(x + c * cols + p, u[c], w[c]);
+        if (mul) {
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            const float2 f = *reinterpret_cast<const float2*>(mul + c * cols + p);
+            u[c] *= f.x, w[c] *= f.y;
+          }
+        }
+        across_columns<C>(u, w, [&](int c, float a, float b) {
+          *reinterpret_cast<float2*>(buf + c * cols + p) = make_float2(a, b);
+        });
+      }
     }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int j = 512 * (wave + 4 * n) + quad_at<true, FULL>(lane, h);
+        const int j = 512 * (wave + WAVES * n) + quad_at<true, FULL>(lane, h);
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         if (j < d) o = *reinterpret_cast<const float4*>(buf + j);
         v[8 * n + 4 * h] = o.x, v[8 * n + 4 * h + 1] = o.y;
@@ -354,7 +383,7 @@ __global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, i
   } else {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int j = 8 * (64 * (wave + 4 * n) + octet_of(lane));
+      const int j = 8 * (64 * (wave + WAVES * n) + octet_of(lane));
       float o[8] = {};
       if (j < d) {
         load8(x + j, o);
@@ -377,7 +406,10 @@ __global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, i
   for (int o = 1; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
   if (lane == 0) red[wave] = mx;
   __syncthreads();
-  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])) * A.turn.norm;
+  mx = red[0];
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) mx = fmaxf(mx, red[i]);
+  mx *= A.turn.norm;
   const int e = int(__float_as_uint(mx) >> 23) - 127;
   const int ue = mx > 0.f && e < 128 ? clampi(e - 7, -100, 100) : 0;
   float up = pow2f(-ue) * A.turn.norm;
@@ -386,7 +418,7 @@ __global__ __launch_bounds__(256) void linear_in(LinearIn A, int table_blocks, i
   if constexpr (C > 0) up *= octet_sign(octet, A.turn.cols);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const int j = 8 * (64 * (wave + 4 * n) + octet);
+    const int j = 8 * (64 * (wave + WAVES * n) + octet);
     float o[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -501,35 +533,31 @@ struct Products {
   }
   // the workers after the first one that hold parts of element j's item: [from, to)
   __device__ __forceinline__ void parts(int j, int& from, int& to) const {
-    const int r = item0 + j / LINEAR_BLOCK - full_items;
+    const int r = item0 + int(unsigned(j) / unsigned(A.block)) - full_items;
     from = to = 0;
     if (r < 0) return;
     from = r * A.ng / per + 1, to = ((r + 1) * A.ng - 1) / per + 1;
     to = to < A.workers ? to : A.workers;
   }
   __device__ __forceinline__ const TP* kept(int worker, int j) const {
-    return static_cast<const TP*>(A.kept) +
-           (int64_t(worker) * 32 * A.nt + in_tile) * LINEAR_BLOCK + j % LINEAR_BLOCK;
+    return static_cast<const TP*>(A.kept) + (int64_t(worker) * 32 * A.nt + in_tile) * A.block +
+           (j & (A.block - 1));  // (128 or 256)
   }
   // eight neighbours
   __device__ __forceinline__ void sum8(int j, float* v) const {
     load8(p + j, v);
     float w[8];
-    if (A.workers == 0) {
-#pragma unroll 4
-      for (int s = 1; s < A.splits; ++s) {
-        load8(p + s * A.stride + j, w);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] += w[k];
-      }
-      return;
-    }
+    if (A.workers == 0) return;
     int from, to;
     parts(j, from, to);
-    for (int s = from; s < to; ++s) {
-      load8(kept(s, j), w);
+    for (; from < to; from += 4) {  // (four at a time: they come one after another otherwise)
+      float u[4][8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] += w[k];
+      for (int i = 0; i < 4; ++i) load8(kept(from + i < to ? from + i : to - 1, j), u[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += from + i < to ? u[i][k] : 0.f;
     }
     if (w_unit) {
       load8(w_unit + j, w);
@@ -539,23 +567,61 @@ struct Products {
   }
   __device__ __forceinline__ float sum1(int j) const {
     float v = float(p[j]);
-    if (A.workers == 0) {
-      for (int s = 1; s < A.splits; ++s) v += float(p[s * A.stride + j]);
-      return v;
-    }
+    if (A.workers == 0) return v;
     int from, to;
     parts(j, from, to);
-    for (int s = from; s < to; ++s) v += float(*kept(s, j));
+    for (; from < to; from += 4) {
+      float u[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = float(*kept(from + i < to ? from + i : to - 1, j));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v += from + i < to ? u[i] : 0.f;
+    }
     return w_unit ? v * w_unit[j] : v;
   }
 };
 
+// The epilogue on the row in LDS, times unit and the sign that its octets are left with: the elements
+// of places p and p + 1 of every column c from c0 on, c1 apart. A loop, and not unrolled: the
+// activations' code is long, a row is over before it comes from memory once (46 us for rows of 14336
+// with 56 copies of it, for 23 rows and more alike).
+template <typename T>
+__device__ __forceinline__ void finish_row(const LinearOut& A, const float* buf, int64_t row,
+                                           int expert, float unit, int p, int c0, int c1) {
+  const int d = int(A.d_out), cols = A.turn.cols;
+  const float* const mul = A.mul ? A.mul + int64_t(expert) * d : nullptr;
+  const float* const bias = A.bias ? A.bias + int64_t(expert) * d : nullptr;
+  const T* const res = A.residual ? static_cast<const T*>(A.residual) + row * A.ldr : nullptr;
+  T* const y = static_cast<T*>(A.y) + row * A.ldy;
+  const float up = unit * octet_sign(p >> 3, cols);
+#pragma unroll 1
+  for (unsigned j = c0 * cols + p; int(j) < d; j += c1 * cols) {
+    const float2 v = *reinterpret_cast<const float2*>(buf + j);
+    float a = v.x * up, b = v.y * up, f, g;
+    if (mul) load2(mul + j, f, g), a *= f, b *= g;
+    if (A.pairs) {
+      if (bias) load2(bias + j, f, g), a += f, b += g;
+      a = activate(a, A.act), b = activate(b, A.act);
+      if (res) load2(res + j, f, g), a += f, b += g;
+      if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint32_t*>(y + j) = uint32_t(f32_bf16(a)) | uint32_t(f32_bf16(b)) << 16;
+      else
+        *reinterpret_cast<float2*>(y + j) = make_float2(a, b);
+    } else {
+      if (bias) a += bias[j], b += bias[j + 1];
+      a = activate(a, A.act), b = activate(b, A.act);
+      if (res) a += load1<T>(res, j), b += load1<T>(res, j + 1);
+      store1<T>(y, j, a);
+      store1<T>(y, j + 1, b);
+    }
+  }
+}
+
 // C columns of a rotated row of whole octets
 template <typename TP, typename T, int C, bool FULL>
-__global__ __launch_bounds__(256) void linear_out(LinearOut A) {
+__global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
   extern __shared__ __attribute__((aligned(16))) float buf[];  // the row
-  __shared__ __attribute__((aligned(16))) float Q[C % 28 == 0 ? 784 : 4];
-  constexpr int N = C >= 4 ? C / 4 : 1;
+  constexpr int THR = threads(C), WAVES = THR / 64, N = (64 * C + THR - 1) / THR;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int d = int(A.d_out), cols = A.turn.cols;
   const int64_t row = blockIdx.x;
@@ -564,14 +630,11 @@ __global__ __launch_bounds__(256) void linear_out(LinearOut A) {
     expert = expert_of(A.offsets, A.n_experts, row);
     if (expert < 0) return;
   }
-  if constexpr (C % 28 == 0) {  // the transposed factor
-    const float* q = A.q28 + int64_t(expert) * 784;
-    for (int i = tid; i < 784; i += 256) Q[(i % 28) * 28 + i / 28] = q[i];
-  }
   const Products<TP> products(A, row, expert);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const int at = 512 * (wave + 4 * n), j = at + 8 * octet_of(lane);
+    const int at = 512 * (wave + WAVES * n), j = at + 8 * octet_of(lane);
+    if (at >= d) break;  // (uniform over the wave)
     float v[8] = {};
     if (j < d) products.sum8(j, v);
     inside_column<1, FULL>(v, lane, cols);
@@ -584,38 +647,27 @@ __global__ __launch_bounds__(256) void linear_out(LinearOut A) {
     }
   }
   __syncthreads();
-  const unsigned p = 2 * tid;
-  if (int(p) >= cols) return;
-  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit *
-                   octet_sign(int(p >> 3), cols);
-  float u[C], w[C];
+  const float unit = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
+  if constexpr (C % 28 == 0) {
+    mix28<C / 28, true>(buf, A.turn.m, A.q28 + int64_t(expert) * 784, wave, WAVES, lane,
+                        [&](int i, float v) { buf[i] = v; });
+    __syncthreads();
+    const int half = cols / 2;  // (a power of two from 4 on)
+    finish_row<T>(A, buf, row, expert, unit, 2 * (tid & (half - 1)), tid / half, THR / half);
+  } else {
+    const int p = 2 * tid;
+    if (p >= cols) return;
+    float u[C], w[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const float2 f = *reinterpret_cast<const float2*>(buf + c * cols + p);
-    u[c] = f.x, w[c] = f.y;
-  }
-  const float* const mul = A.mul ? A.mul + int64_t(expert) * d : nullptr;
-  const float* const bias = A.bias ? A.bias + int64_t(expert) * d : nullptr;
-  const T* const res = A.residual ? static_cast<const T*>(A.residual) + row * A.ldr : nullptr;
-  T* const y = static_cast<T*>(A.y) + row * A.ldy;
-  across_columns<C>(u, w, Q, [&](int c, float a, float b) {
-    const unsigned j = c * cols + p;
-    a *= up, b *= up;
-    if (!A.pairs) {
-      store1<T>(y, j, finish<T>(a, j, mul, bias, res, A.act));
-      store1<T>(y, j + 1, finish<T>(b, j + 1, mul, bias, res, A.act));
-      return;
+    for (int c = 0; c < C; ++c) {
+      const float2 f = *reinterpret_cast<const float2*>(buf + c * cols + p);
+      u[c] = f.x, w[c] = f.y;
     }
-    float f, g;
-    if (mul) load2(mul + j, f, g), a *= f, b *= g;
-    if (bias) load2(bias + j, f, g), a += f, b += g;
-    if (A.act != KRONQ_ACT_NONE) a = activate(a, A.act), b = activate(b, A.act);
-    if (res) load2(res + j, f, g), a += f, b += g;
-    if constexpr (sizeof(T) == 2)
-      *reinterpret_cast<uint32_t*>(y + j) = uint32_t(f32_bf16(a)) | uint32_t(f32_bf16(b)) << 16;
-    else
-      *reinterpret_cast<float2*>(y + j) = make_float2(a, b);
-  });
+    across_columns<C>(u, w, [&](int c, float a, float b) {
+      *reinterpret_cast<float2*>(buf + c * cols + p) = make_float2(a, b);
+    });
+    finish_row<T>(A, buf, row, expert, unit, p, 0, 1);  // (of what this thread has put there)
+  }
 }
 
 // Rows without a transform, and transforms whose columns are shorter than an octet (cols: 1, 2 or 4
@@ -659,11 +711,12 @@ __global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
 
 template <typename T>
 int in_typed(const LinearIn& a, hipStream_t s) {
-  const int64_t table_blocks = a.table ? cdiv(a.w_rows, 8) : 0;
+  const int cc = a.turn.rotate ? int(a.d_in / a.turn.cols) : 0;
+  const int64_t table_blocks = a.table ? cdiv(a.w_rows, threads(cc) / 32) : 0;
   const int64_t lead = cdiv(table_blocks + (a.offsets ? 1 : 0), 8) * 8;
   const dim3 grid(static_cast<unsigned>(lead + cdiv(a.n_rows, 256) * 256));
 #define KQ_IN(C_, N_, F_)                                                                            \
-  launch("linear_in", linear_in<T, C_, N_, F_>, grid, dim3(256), C_ ? size_t(a.d_in) * 4 : 0, s, a, \
+  launch("linear_in", linear_in<T, C_, N_, F_>, grid, dim3(threads(C_)), C_ ? size_t(a.d_in) * 4 : 0, s, a, \
          int(table_blocks), int(lead))
   if (!a.turn.rotate) {
     const int64_t n = cdiv(a.d_in, 2048);
@@ -671,7 +724,7 @@ int in_typed(const LinearIn& a, hipStream_t s) {
                                                                                   : KQ_IN(0, 16, false);
   }
   const bool full = a.turn.cols == 512;
-  switch (a.d_in / a.turn.cols) {
+  switch (cc) {
     case 1:
       return full ? KQ_IN(1, 1, true) : KQ_IN(1, 1, false);
     case 2:
@@ -687,9 +740,9 @@ int in_typed(const LinearIn& a, hipStream_t s) {
     case 64:
       return KQ_IN(64, 16, true);
     case 28:
-      return full ? KQ_IN(28, 7, true) : KQ_IN(28, 7, false);
+      return full ? KQ_IN(28, 2, true) : KQ_IN(28, 2, false);
     default:
-      return KQ_IN(56, 14, true);
+      return KQ_IN(56, 4, true);
   }
 #undef KQ_IN
 }
@@ -704,7 +757,7 @@ int out_typed(LinearOut a, hipStream_t s) {
   if (!a.turn.rotate || a.turn.cols < 8)
     return launch("linear_out", linear_out_any<TP, T>, grid, dim3(256), 0, s, a);
 #define KQ_OUT(C_, F_) \
-  launch("linear_out", linear_out<TP, T, C_, F_>, grid, dim3(256), size_t(a.d_out) * 4, s, a)
+  launch("linear_out", linear_out<TP, T, C_, F_>, grid, dim3(threads(C_)), size_t(a.d_out) * 4, s, a)
   const bool full = a.turn.cols == 512;
   switch (a.d_out / a.turn.cols) {
     case 1:
