@@ -145,50 +145,54 @@ __device__ __forceinline__ void wait_vm() {  // s_waitcnt vmcnt(N), the other co
   __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
 }
 
-// this lane's codes of half a group: one chunk of 32
+// this lane's codes of a group: two chunks of 32
 template <int BITS>
-struct Chunk {
-  uint32_t w[BITS];
-};
-template <int BITS>
-__device__ __forceinline__ Chunk<BITS> load_chunk(const uint32_t* p) {
-  Chunk<BITS> c;
-  if constexpr (BITS == 2) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    c.w[0] = v.x, c.w[1] = v.y;
-  } else if constexpr (BITS == 3) {
-    c.w[0] = p[0], c.w[1] = p[1], c.w[2] = p[2];
+__device__ __forceinline__ void load_codes(uint32_t* w, const uint32_t* p) {
+  if constexpr (BITS == 3) {
+#pragma unroll
+    for (int k = 0; k < 6; k += 2) {
+      const uint2 v = *reinterpret_cast<const uint2*>(p + k);
+      w[k] = v.x, w[k + 1] = v.y;
+    }
   } else {
 #pragma unroll
-    for (int k = 0; k < BITS; k += 4) {
+    for (int k = 0; k < 2 * BITS; k += 4) {
       const uint4 v = *reinterpret_cast<const uint4*>(p + k);
-      c.w[k] = v.x, c.w[k + 1] = v.y, c.w[k + 2] = v.z, c.w[k + 3] = v.w;
+      w[k] = v.x, w[k + 1] = v.y, w[k + 2] = v.z, w[k + 3] = v.w;
     }
   }
-  return c;
 }
 
 // A workgroup of four waves takes 128 RT rows of W (32 RT a wave) and a tile of NT units of rows of
 // x'; a lane holds the codes of RT rows of W and half of the columns, 64 of them a stage. x' comes
 // through LDS: a stage is 64 columns (half a group, a chunk of each lane's codes) of NT units in
 // PLANES planes, pieces of 4 KB that the waves bring straight to LDS, in fragment order as they
-// stand, through a ring of four stages. One barrier a stage, in its middle: it publishes the next
-// stage and frees the buffer of the one before, which the loads of three stages on then fill;
-// operands are read one step of 16 columns ahead.
+// stand, through a ring of R stages. One barrier a stage, in its middle: it publishes the next stage
+// and frees the buffer of the one before, which the loads of R - 1 stages on then fill; operands are
+// read one step of 16 columns ahead.
 //   SCALED, NT = 4, RT = 2 (many rows): the matrix instructions bound it. Two workgroups per CU (64 KB
 //     of LDS and 256 registers a lane each), so that one wave's spreading of codes runs beside the
 //     other's matrix instructions. Results leave as fp16 (linear_out multiplies by the units of the
 //     rows of W).
 //   PLANES = 2, NT = 2, RT = 2: the same for fp32 results.
-//   RT = 1 (few rows): the codes' way from memory bounds it; four workgroups per CU keep the loads of
-//     16 waves out at a time.
-constexpr int per_cu(int rt) { return rt == 2 ? 2 : 4; }
+//   RT = 1 (few rows): the codes' way from memory bounds it, with three or four workgroups per CU.
+// A lane reads its row of W in batches, of a whole 128-byte line with RT = 1: chunk by chunk the lines
+// left the L1 between two reads of one, and came from L2 up to four times. The fp32 scales and zeros
+// (not SCALED) come through LDS eight groups at a time for the same reason: 32 rows lie in 32 lines of
+// either. (8 experts of 14336 x
+// 4096 at 4 bits with 32 rows: 76 us that way, 66 now.)
+constexpr int per_cu(int nt, int rt) { return rt == 2 ? 2 : nt == 2 ? 3 : 4; }
 
 template <int BITS, int NT, int PLANES, int RT, bool SCALED>
-__global__ __launch_bounds__(256, per_cu(RT)) void linear_ring(MmArgs A) {
-  constexpr int NP = NT * PLANES, STAGE = NP * 1024, R = 4, BLOCK = 128 * RT;  // (STAGE: dwords)
-  static_assert(!SCALED || PLANES == 1, "fp32 results take exact weights");
-  __shared__ __attribute__((aligned(16))) uint32_t lds[R * STAGE];
+__global__ __launch_bounds__(256, per_cu(NT, RT)) void linear_ring(MmArgs A) {
+  constexpr int NP = NT * PLANES, STAGE = NP * 1024, BLOCK = 128 * RT;  // (STAGE: dwords)
+  constexpr int R = NP == 1 ? 8 : 4;  // stages of the ring
+  // groups of a batch of codes: 16 words a lane with RT = 1 (12 with 3 bits), 8 with RT = 2
+  constexpr int BG = RT == 1 ? (BITS == 2 ? 4 : BITS == 8 ? 1 : 2) : BITS == 2 ? 2 : 1;
+  constexpr int SG = 8;  // groups of scales and zeros in LDS
+  // the ring, then {scale, fp16 pair of -(1024 + zero)} by group and row (one array: with a second one
+  // the compiler waits for all loads to LDS before each read)
+  __shared__ __attribute__((aligned(16))) uint32_t lds[R * STAGE + (SCALED ? 0 : 2 * SG * BLOCK)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Workers that share an XCD (workgroup % 8) stand next to one another in the deal, so that the x'
   // of a tile is read through one L2, by all blocks of W at about the same time.
@@ -241,71 +245,104 @@ __global__ __launch_bounds__(256, per_cu(RT)) void linear_ring(MmArgs A) {
       wr[i] = int64_t(t.expert) * A.d_out + (n < A.d_out ? n : A.d_out - 1);
       wp[i] = A.packed + wr[i] * A.ldp + (int64_t(g0) * 4 + (lane >> 5) * 2) * BITS;
     }
-    Chunk<BITS> cw[2][RT];
-    uint32_t sz1[RT];  // of the next group
-    float sc[RT], sc1[RT];
-    auto codes = [&](int st, int h) {  // h = st & 1
-      st = st < nst ? st : nst - 1;
+    const int ngr = g1 - g0;
+    uint32_t cw[RT][BG * 2 * BITS], next[RT][BG * 2 * BITS];
+    auto codes = [&](uint32_t (&w)[RT][BG * 2 * BITS], int gb) {  // the batch of the range's group gb
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
-        cw[h][i] = load_chunk<BITS>(wp[i] + int64_t(st >> 1) * 4 * BITS + (st & 1) * BITS);
+      for (int k = 0; k < BG; ++k)
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+          load_codes<BITS>(w[i] + k * 2 * BITS,
+                           wp[i] + int64_t(gb + k < ngr ? gb + k : ngr - 1) * 4 * BITS);
     };
-    auto params = [&](int gi) {  // of the group gi of this range
-      const int g = g0 + gi < g1 ? g0 + gi : g1 - 1;
+    uint32_t sz[RT], sz1[RT];  // SCALED: of this group and the next one
+    auto table = [&](int gi) {
+      const int g = g0 + (gi < ngr ? gi : ngr - 1);
+#pragma unroll
+      for (int i = 0; i < RT; ++i) sz1[i] = A.table[int64_t(g) * A.w_rows + wr[i]];
+    };
+    // otherwise: this thread's row and four of the eight groups (per 128 rows)
+    float sc[RT], ps[SCALED ? 1 : RT][4], pz[SCALED ? 1 : RT][4];
+    const int64_t brow = int64_t(t.expert) * A.d_out + int64_t(rb) * BLOCK;
+    auto fetch = [&](int gi) {
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
-        if constexpr (SCALED) {
-          sz1[i] = A.table[int64_t(g) * A.w_rows + wr[i]];
-        } else {
-          const int64_t at = wr[i] * A.ldsz + unsigned(g) / unsigned(A.gpq);
-          sc1[i] = A.scales[at];
-          sz1[i] = __float_as_uint(A.zeros[at]);
+        const int r = int(threadIdx.x >> 1) + 128 * i;
+        const int64_t n = int64_t(rb) * BLOCK + r;
+        const int64_t at = (n < A.d_out ? brow + r : brow) * A.ldsz;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int g = gi + 4 * int(threadIdx.x & 1) + k;
+          const unsigned q = unsigned(g0 + (g < ngr ? g : ngr - 1)) / unsigned(A.gpq);
+          ps[i][k] = A.scales[at + q], pz[i][k] = A.zeros[at + q];
         }
       }
     };
+    uint2* const params = reinterpret_cast<uint2*>(lds + R * STAGE);  // [group % SG][row]
+    auto put = [&]() {
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const _Float16 nz = _Float16(-1024.f - pz[i][k]);
+          params[(4 * (threadIdx.x & 1) + k) * BLOCK + (threadIdx.x >> 1) + 128 * i] =
+              make_uint2(__float_as_uint(ps[i][k]), u2(f16x2_t{nz, nz}));
+        }
+    };
     f32x16_t acc[NT][RT] = {}, sum[SCALED ? 1 : NT][SCALED ? 1 : RT] = {};
-    params(0);
-    codes(0, 0);
+    if constexpr (SCALED)
+      table(0);
+    else
+      fetch(0);
+    codes(cw, 0);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int st = 0; st < 3; ++st) issue(st);
+    for (int st = 0; st < R - 1; ++st) issue(st);
+    if constexpr (!SCALED) put();
     u32x4_t a[2][NP];
     auto frags = [&](int st, int q) {
       const uint32_t* buf = lds + (st & (R - 1)) * STAGE + lane * 4 + q * 256;
 #pragma unroll
       for (int i = 0; i < NP; ++i) a[q & 1][i] = *reinterpret_cast<const u32x4_t*>(buf + i * 1024);
     };
-    uint32_t z[RT];
-    auto stage = [&](int st, auto hc) {
-      constexpr int h = decltype(hc)::value;
-      codes(st + 1, h ^ 1);
-      if constexpr (h == 0) {
+    // stage u of a batch
+    auto stage = [&](int st, auto uc) {
+      constexpr int u = decltype(uc)::value, h = u & 1;
+      const int gi = st >> 1;
+      if constexpr (h == 0 && SCALED) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) sz[i] = sz1[i];
+        table(gi + 1);
+      }
+      if constexpr (h == 0 && !SCALED) {
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-          z[i] = sz1[i], sc[i] = sc1[i];
-          if constexpr (!SCALED) {
-            const _Float16 nz = _Float16(-1024.f - __uint_as_float(sz1[i]));
-            z[i] = u2(f16x2_t{nz, nz});
-          }
+          const uint2 v = params[(gi & (SG - 1)) * BLOCK + 32 * (RT * wave + i) + (lane & 31)];
+          sc[i] = __uint_as_float(v.x), sz[i] = v.y;
         }
-        params((st >> 1) + 1);
+        if ((gi & (SG - 1)) == 0 && gi + SG < ngr) fetch(gi + SG);
       }
+      // (every wave has read the last of the eight groups before the barrier of this group's first
+      // stage, and reads the next one's after that of its second)
+      if constexpr (h == 1 && !SCALED)
+        if ((gi & (SG - 1)) == SG - 1 && gi + 1 < ngr) put();
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         if (q == 2) {
-          // the next stage's loads have landed (the NP of the one after it may be out, and what this
-          // wave has requested of codes before and after those, RT loads at least each)
-          wait_vm<NP + 2 * RT>();
+          // the next stage's loads have landed (those of the R - 3 after it may be out)
+          wait_vm<(R - 3) * NP>();
+          if constexpr (h == 1 && !SCALED) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           __builtin_amdgcn_s_barrier();
-          issue(st + 3);
+          issue(st + R - 1);
           __builtin_amdgcn_sched_barrier(0);
         }
         frags(q < 3 ? st : st + 1, (q + 1) & 3);
         u32x4_t b[RT];
 #pragma unroll
         for (int k = 0; k < RT; ++k)
-          b[k] = SCALED ? spread<BITS>(cw[h][k].w, q, z[k]) : spread_int<BITS>(cw[h][k].w, q, z[k]);
+          b[k] = SCALED ? spread<BITS>(cw[k] + u * BITS, q, sz[k])
+                        : spread_int<BITS>(cw[k] + u * BITS, q, sz[k]);
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -333,12 +370,29 @@ __global__ __launch_bounds__(256, per_cu(RT)) void linear_ring(MmArgs A) {
         }
       }
     };
-    wait_vm<2 * NP>();
+    wait_vm<(R - 2) * NP>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     frags(0, 0);
-    for (int st = 0; st < nst; st += 2) {
-      stage(st, std::integral_constant<int, 0>{});
-      stage(st + 1, std::integral_constant<int, 1>{});
+    for (int gb = 0; gb < ngr; gb += BG) {
+      codes(next, gb + BG);
+      auto pair = [&](auto kc) {
+        constexpr int k = decltype(kc)::value;
+        stage(2 * (gb + k), std::integral_constant<int, 2 * k>{});
+        stage(2 * (gb + k) + 1, std::integral_constant<int, 2 * k + 1>{});
+      };
+      pair(std::integral_constant<int, 0>{});
+      if constexpr (BG > 1) {
+        if (gb + 1 < ngr) pair(std::integral_constant<int, 1>{});
+      }
+      if constexpr (BG > 2) {
+        if (gb + 2 < ngr) pair(std::integral_constant<int, 2>{});
+        if (gb + 3 < ngr) pair(std::integral_constant<int, 3>{});
+      }
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int k = 0; k < BG * 2 * BITS; ++k) cw[i][k] = next[i][k];
     }
     wait_vm<0>();  // (loads past the end still write to LDS)
     __builtin_amdgcn_s_barrier();
@@ -394,7 +448,7 @@ Plan make_plan(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts, i
   p.block = 128 * p.rt;
   p.tiles = n_experts == 1 ? cdiv(n_rows, 32 * p.nt) : most_tiles(n_rows, n_experts, p.nt);
   p.row_blocks = cdiv(d_out, p.block);
-  p.workers = device_cus() / 8 * 8 * per_cu(p.rt);
+  p.workers = device_cus() / 8 * 8 * per_cu(p.nt, p.rt);
   // fp16 results: below 2^8 (x') times 2.5 (|c - z| < 1280 of at most 2^-9) times d_in
   p.down = 1.f;
   while (p.scaled && 640.f * float(d_in) * p.down > 65000.f) p.down *= 0.5f;

@@ -237,20 +237,24 @@ __device__ __forceinline__ void across_columns(float (&x)[C], float (&y)[C], Put
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
+// A lane's share of the factor (or its transpose) as the A operand of mix28
+template <bool TRANS>
+__device__ __forceinline__ void load28(float (&q)[14], const float* __restrict__ q28, int lane) {
+#pragma unroll
+  for (int s = 0; s < 14; ++s) {
+    const int k = 2 * s + (lane >> 5), n = lane & 31, a = n < 28 ? n : 27;
+    q[s] = q28[TRANS ? k * 28 + a : a * 28 + k];  // (rows 28 to 31 are not used)
+  }
+}
+
 // The 28 x 28 factor over the segments of m elements of the row in LDS, on the fp32 matrix cores (as
 // multiply-adds of a thread's own elements it took three times as long: two chains of 28 at a time),
 // and, for m = 1024 (B = 2), the stage of stride 512 that a column of 512 leaves out. A wave takes
 // 32 places of every segment at a time; place(i, v): element i of the row has become v.
-template <int B, bool TRANS, typename Place>
-__device__ __forceinline__ void mix28(const float* buf, int m, const float* __restrict__ q28,
-                                      int wave, int waves, int lane, Place place) {
+template <int B, typename Place>
+__device__ __forceinline__ void mix28(const float* buf, int m, const float (&q)[14], int wave,
+                                      int waves, int lane, Place place) {
   const int n = lane & 31, half = lane >> 5;
-  float q[14];
-#pragma unroll
-  for (int s = 0; s < 14; ++s) {
-    const int k = 2 * s + half, a = n < 28 ? n : 27;
-    q[s] = q28[TRANS ? k * 28 + a : a * 28 + k];  // (rows 28 to 31 are not used)
-  }
   const int cols = B == 2 ? 512 : m;
   for (int p0 = 32 * wave; p0 < cols; p0 += 32 * waves) {
     const int p = p0 + n, pc = p < cols ? p : cols - 1;
@@ -331,6 +335,8 @@ __global__ __launch_bounds__(threads(C)) void linear_in(LinearIn A, int table_bl
   if constexpr (C > 0) {
     const int cols = A.turn.cols;
     if constexpr (C % 28 == 0) {
+      float q[14];
+      load28<false>(q, A.q28 + int64_t(expert) * 784, lane);
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         const int j = 8 * (tid + THR * n);
@@ -348,8 +354,7 @@ __global__ __launch_bounds__(threads(C)) void linear_in(LinearIn A, int table_bl
       }
       __syncthreads();
       // (in place: a wave reads all of its 32 places before it writes them)
-      mix28<C / 28, false>(buf, A.turn.m, A.q28 + int64_t(expert) * 784, wave, WAVES, lane,
-                           [&](int i, float v) { buf[i] = v; });
+      mix28<C / 28>(buf, A.turn.m, q, wave, WAVES, lane, [&](int i, float v) { buf[i] = v; });
     } else {
       const unsigned p = 2 * tid;
       if (int(p) < cols) {
@@ -630,6 +635,8 @@ __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
     expert = expert_of(A.offsets, A.n_experts, row);
     if (expert < 0) return;
   }
+  float q[14];
+  if constexpr (C % 28 == 0) load28<true>(q, A.q28 + int64_t(expert) * 784, lane);
   const Products<TP> products(A, row, expert);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -649,8 +656,7 @@ __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
   __syncthreads();
   const float unit = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
   if constexpr (C % 28 == 0) {
-    mix28<C / 28, true>(buf, A.turn.m, A.q28 + int64_t(expert) * 784, wave, WAVES, lane,
-                        [&](int i, float v) { buf[i] = v; });
+    mix28<C / 28>(buf, A.turn.m, q, wave, WAVES, lane, [&](int i, float v) { buf[i] = v; });
     __syncthreads();
     const int half = cols / 2;  // (a power of two from 4 on)
     finish_row<T>(A, buf, row, expert, unit, 2 * (tid & (half - 1)), tid / half, THR / half);
