@@ -11,6 +11,7 @@
 // ([token / 4][word][token % 4]) so that a lane's load brings it four tokens of its channels.
 // params [page][kv head][key, value][token]: scale (bf16, upper half) and zero (lower half).
 #include <cmath>
+#include <type_traits>
 
 #include "kq_common.hpp"
 #include "kq_fwht.hpp"
@@ -140,9 +141,11 @@ __global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
 
 // ---- attention -----------------------------------------------------------------------------------
 // For one sequence and kv head, the new tokens' queries of the heads that share it are rows: row
-// i G + g is token i, head g of G. A workgroup of four waves takes 16 MQ rows and a range of the
-// cached tokens, which its waves walk in turn, 32 tokens at a time, each with its own running
-// maximum and sums; they meet in LDS once at the end. One pass over the cache:
+// i G + g is token i, head g of G. A wave takes 16 MQ rows and walks a range of the cached tokens, 32
+// at a time, one pass with a running maximum and sums. The four waves of a workgroup
+//   BY_ROWS (prompts): take different rows and the same tokens; each ends with its own rows;
+//   otherwise (few rows: decoding): take the same rows and tokens in turn, and meet in LDS at the end.
+// Beside that a range of tokens is split over workgroups where rows are few; attention_join ends that.
 //   scores   S[token][row] = K q on v_mfma_f32_16x16x32_f16, twice 16 tokens: a lane spreads the
 //            codes of its token and channels straight from the loaded words. A code left at bit 0
 //            or 4 of its half word is the subnormal fp16 c 2^-24 or c 2^-20, so a pair of codes
@@ -196,6 +199,21 @@ __device__ __forceinline__ void store_row(uint16_t* o, float (&x)[2], int lane, 
   if constexpr (DIM == 128) o[lane + 64] = f32_bf16(x[1]);
 }
 
+// the butterfly stages over lanes 0 to 15 (of each 16): channels 8 n + d of row_dim 128 and, with
+// n & 7 and 4 (n >> 3) + d, of 64
+template <int ND>
+__device__ __forceinline__ void turn16(float (&x)[ND], int n) {
+  const float s0 = (n & 1) ? -1.f : 1.f, s1 = (n & 2) ? -1.f : 1.f;
+  const float s2 = (n & 4) ? -1.f : 1.f, s3 = (n & 8) ? -1.f : 1.f;
+#pragma unroll
+  for (int e = 0; e < ND; ++e) {
+    x[e] = fmaf(x[e], s0, dpp_mov<0xB1>(x[e]));
+    x[e] = fmaf(x[e], s1, dpp_mov<0x4E>(x[e]));
+    x[e] = fmaf(x[e], s2, dpp_mov<0x1B>(dpp_mov<0x141>(x[e])));
+    x[e] = fmaf(x[e], s3, dpp_mov<0x128>(x[e]));
+  }
+}
+
 __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a),
                                                 __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
@@ -208,12 +226,13 @@ struct KvTile {
   int bad;  // halves on pages that do not exist
 };
 
-template <int DIM, int MQ>
-__global__ __launch_bounds__(256) void cache_attention(AttnArgs A) {
+template <int DIM, int MQ, bool BY_ROWS>
+__global__ __launch_bounds__(256, MQ == 1 ? 2 : 2) void cache_attention(AttnArgs A) {
   constexpr int NJ = DIM / 32;       // words of a key row a lane takes, matrix steps per score
   constexpr int ND = DIM / 16;       // output blocks of 16 channels
   constexpr int WPR = DIM / 8;       // words per row
-  constexpr int ROWS = 16 * MQ, LD = DIM + 4;
+  constexpr int ROWS = 16 * MQ, TILE = BY_ROWS ? 4 * ROWS : ROWS, LD = DIM + 4;
+  constexpr int STEP = BY_ROWS ? 32 : 128;  // tokens from one of a wave's tiles to the next
   extern __shared__ __attribute__((aligned(16))) float sm[];  // [wave][row][LD], [wave][row][2]
   float* sml = sm + 4 * ROWS * LD;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -224,20 +243,22 @@ __global__ __launch_bounds__(256) void cache_attention(AttnArgs A) {
   const int nt = int(A.n_tokens);
   int q0 = b, q1 = b + 1;
   if (A.starts) {
-    q0 = A.starts[b], q1 = A.starts[b + 1];
+    q0 = __builtin_amdgcn_readfirstlane(A.starts[b]);
+    q1 = __builtin_amdgcn_readfirstlane(A.starts[b + 1]);
     q0 = q0 < 0 ? 0 : q0 > nt ? nt : q0;
     q1 = q1 < q0 ? q0 : q1 > nt ? nt : q1;
   }
   const int nq = q1 - q0, G = A.group, nrows = nq * G;
-  int len = A.lengths[b];
+  int len = __builtin_amdgcn_readfirstlane(A.lengths[b]);
   const int most = A.table_pages << A.page_log;
   len = len < 0 ? 0 : len > most ? most : len;
   const int* table = A.table + int64_t(b) * A.ldt;
   const int page_mask = (1 << A.page_log) - 1;
   // later rows see more tokens: they go first
-  const int tiles = (nrows + ROWS - 1) / ROWS;
+  const int tiles = (nrows + TILE - 1) / TILE;
   for (int tile = tiles - 1 - int(blockIdx.x / A.splits); tile >= 0; tile -= A.tiles) {
-    const int row0 = tile * ROWS;
+    const int row0 = tile * TILE + (BY_ROWS ? wave * ROWS : 0);
+    if (BY_ROWS && row0 >= nrows) continue;
     const int end_row = row0 + ROWS < nrows ? row0 + ROWS : nrows;
     // tokens that the tile's first and last rows see
     const int see0 = len - nq + row0 / G + 1, see1 = len - nq + (end_row - 1) / G + 1;
@@ -300,6 +321,7 @@ __global__ __launch_bounds__(256) void cache_attention(AttnArgs A) {
       }
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
+      __builtin_amdgcn_sched_barrier(0);
       qsum[i] = sum * 0x1p-24f;
       qs[i] = A.scale * __uint_as_float(uint32_t(127 + ue) << 23) * 0x1p24f;
       if (A.rotate) qs[i] *= DIM == 128 ? 0.08838834764831845f : 0.125f;
@@ -310,20 +332,29 @@ __global__ __launch_bounds__(256) void cache_attention(AttnArgs A) {
 #pragma unroll
     for (int i = 0; i < MQ; ++i) m[i] = -1e30f, l[i] = 0.f, zs[i] = 0.f;
 
-    auto load = [&](KvTile<NJ>& T, int t0) {
+    // The pages of this wave's next 32 tiles, one of their halves of 16 a lane: read one by one, each
+    // tile would wait for its page before it could ask for its codes.
+    const int first = beg_t + (BY_ROWS ? 0 : 32 * wave);
+    int pages = 0, k0 = -32;
+    // past the end: the last tokens again, masked below
+    const unsigned at_k = n * WPR + g4 * NJ, at_v = (g4 * WPR + (n & (WPR - 1))) * 4, at_p = 4 * g4;
+    auto token = [&](int t) { return t < end ? t : (end - 1) & ~15; };
+    auto load = [&](KvTile<NJ>& T, int k) {  // this wave's tile k
+      if (k >= k0 + 32) {
+        k0 = k;
+        pages = table[token(first + STEP * (k + (lane >> 1)) + 16 * (lane & 1)) >> A.page_log];
+      }
       T.bad = 0;
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
-        int t = t0 + 16 * f;
-        t = t < end ? t : (end - 1) & ~15;  // past the end: the last tokens again, masked below
-        int p = table[t >> A.page_log];
+        const int t = token(first + STEP * k + 16 * f);
+        int p = __builtin_amdgcn_readlane(pages, 2 * (k - k0) + f);
         if (p < 0 || p >= A.n_pages) p = 0, T.bad |= 1 << f;
-        const int off = t & page_mask;
-        const int64_t ph = (int64_t(p) * A.n_kv + h) * 2;
-        const uint32_t* kc = A.codes + ((ph << A.page_log) + off + n) * WPR + g4 * NJ;
-        const uint32_t* vc = A.codes + (((ph + 1) << A.page_log) + off) * WPR +
-                             (g4 * WPR + (n & (WPR - 1))) * 4;
-        const uint32_t* pp = A.params + (ph << A.page_log) + off + 4 * g4;
+        // (uniform bases and the lane's 32-bit offsets: no 64-bit address is held per lane)
+        const int64_t slot = (((int64_t(p) * A.n_kv + h) * 2) << A.page_log) + (t & page_mask);
+        const uint32_t* const kc = A.codes + slot * WPR + at_k;
+        const uint32_t* const vc = A.codes + (slot + (1 << A.page_log)) * WPR + at_v;
+        const uint32_t* const pp = A.params + slot + at_p;
         if constexpr (NJ == 4) {
           const uint4 w = *reinterpret_cast<const uint4*>(kc);
           T.k[f][0] = w.x, T.k[f][1] = w.y, T.k[f][2] = w.z, T.k[f][3] = w.w;
@@ -340,7 +371,9 @@ __global__ __launch_bounds__(256) void cache_attention(AttnArgs A) {
       }
     };
 
-    auto work = [&](const KvTile<NJ>& T, int t0) {
+    // CUT: some of the tokens do not count, or not for every row
+    auto work = [&](const KvTile<NJ>& T, int t0, auto cut_c) {
+      constexpr bool CUT = decltype(cut_c)::value;
       f32x4_t s[MQ][2] = {};
 #pragma unroll
       for (int f = 0; f < 2; ++f)
@@ -351,39 +384,40 @@ __global__ __launch_bounds__(256) void cache_attention(AttnArgs A) {
 #pragma unroll
           for (int i = 0; i < MQ; ++i) s[i][f] = mfma16(a, qf[i][j], s[i][f]);
         }
-      // scales and zeros of this lane's tokens 16 f + 4 g4 + r
-      float ks[2][4], kz[2][4], vs[2][4], vz[2][4], svm = 0.f;
-      const bool cut = t0 + 32 > end_t || T.bad;  // (uniform)
+      __builtin_amdgcn_sched_barrier(0);  // (else all codes are spread ahead, and registers spill)
+      // does this lane's token 16 f + 4 g4 + r count at all
+      auto counts = [&](int f, int r) {
+        return !CUT || (t0 + 16 * f + 4 * g4 + r < end_t && !(T.bad >> f & 1));
+      };
+      // its value scale (what stands in a place that does not count is nothing)
+      auto value_scale = [&](int f, int r) {
+        const float v = __uint_as_float(T.vp[f][r] & 0xFFFF0000u);
+        return counts(f, r) ? v : 0.f;
+      };
+      float svm = 0.f;
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) svm = fmaxf(svm, value_scale(f, r));
+      bool up = svm > 128.f * sigma;
+      float top[MQ];
+#pragma unroll
+      for (int i = 0; i < MQ; ++i) top[i] = -INFINITY;
 #pragma unroll
       for (int f = 0; f < 2; ++f)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          ks[f][r] = __uint_as_float(T.kp[f][r] & 0xFFFF0000u), kz[f][r] = float(T.kp[f][r] & 0xFFu);
-          vs[f][r] = __uint_as_float(T.vp[f][r] & 0xFFFF0000u), vz[f][r] = float(T.vp[f][r] & 0xFFu);
-          if (cut && (t0 + 16 * f + 4 * g4 + r >= end_t || (T.bad >> f & 1)))
-            vs[f][r] = 0.f, vz[f][r] = 0.f;  // (whatever stands there counts for nothing)
-          svm = fmaxf(svm, vs[f][r]);
-        }
-      const bool mask = cut || t0 + 32 > see0;
-      bool up = svm > 128.f * sigma;
-      float top[MQ];
+          const float ks = __uint_as_float(T.kp[f][r] & 0xFFFF0000u), kz = float(T.kp[f][r] & 0xFFu);
 #pragma unroll
-      for (int i = 0; i < MQ; ++i) {
-        top[i] = -INFINITY;
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float v = fmaf(-kz[f][r], qsum[i], s[i][f][r]) * (ks[f][r] * qs[i]);
-            if (mask) {
-              const int t = t0 + 16 * f + 4 * g4 + r;
-              if (t >= see[i] || t >= end_t || (T.bad >> f & 1)) v = -INFINITY;
-            }
+          for (int i = 0; i < MQ; ++i) {
+            float v = fmaf(-kz, qsum[i], s[i][f][r]) * (ks * qs[i]);
+            if (CUT && (t0 + 16 * f + 4 * g4 + r >= see[i] || !counts(f, r))) v = -INFINITY;
             s[i][f][r] = v;
             top[i] = fmaxf(top[i], v);
           }
-        up |= top[i] > m[i] + 7.f;
-      }
+        }
+#pragma unroll
+      for (int i = 0; i < MQ; ++i) up |= top[i] > m[i] + 7.f;
       if (__any(up)) {  // new references
         float sn = svm;
 #pragma unroll
@@ -408,30 +442,31 @@ __global__ __launch_bounds__(256) void cache_attention(AttnArgs A) {
             for (int r = 0; r < 4; ++r) acc[i][d][r] *= fr[r];
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
       u32x4_t pf[MQ];
 #pragma unroll
       for (int f = 0; f < 2; ++f)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) vs[f][r] *= sinv;
+        for (int r = 0; r < 4; r += 2) {
+          const float s0 = value_scale(f, r) * sinv, s1 = value_scale(f, r + 1) * sinv;
+          const float z0 = float(T.vp[f][r] & 0xFFu), z1 = float(T.vp[f][r + 1] & 0xFFu);
 #pragma unroll
-      for (int i = 0; i < MQ; ++i)
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-          for (int r = 0; r < 4; r += 2) {
+          for (int i = 0; i < MQ; ++i) {
             const float p0 = __builtin_amdgcn_exp2f(s[i][f][r] - m[i]);
             const float p1 = __builtin_amdgcn_exp2f(s[i][f][r + 1] - m[i]);
             l[i] += p0 + p1;
-            float w0 = p0 * vs[f][r], w1 = p1 * vs[f][r + 1];
-            if (mask) {  // a hidden token's value may read as NaN
+            float w0 = p0 * s0, w1 = p1 * s1;
+            if (CUT) {  // a hidden token's value may read as NaN
               if (s[i][f][r] == -INFINITY) w0 = 0.f;
               if (s[i][f][r + 1] == -INFINITY) w1 = 0.f;
             }
-            zs[i] = fmaf(w0, vz[f][r], zs[i]);
-            zs[i] = fmaf(w1, vz[f][r + 1], zs[i]);
+            zs[i] = fmaf(w0, z0, zs[i]);
+            zs[i] = fmaf(w1, z1, zs[i]);
             pf[i][2 * f + (r >> 1)] =
                 __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{w0, w1}, f16x2_t));
           }
+        }
+      __builtin_amdgcn_sched_barrier(0);
       // value codes: channel 8 n + d, pairs of tokens
       if constexpr (DIM == 128) {
 #pragma unroll
@@ -467,29 +502,78 @@ __global__ __launch_bounds__(256) void cache_attention(AttnArgs A) {
       }
     };
 
-    // this wave's tiles of 32 tokens, the next one loaded meanwhile
-    if (beg_t + 32 * wave < end_t) {
-      KvTile<NJ> T[2];
-      load(T[0], beg_t + 32 * wave);
-      for (int t0 = beg_t + 32 * wave;;) {
-        const int t1 = t0 + 128;
-        if (t1 < end_t) load(T[1], t1);
-        work(T[0], t0);
-        if (t1 >= end_t) break;
-        t0 = t1 + 128;
-        if (t0 < end_t) load(T[0], t0);
-        work(T[1], t1);
-        if (t0 >= end_t) break;
+    auto turn = [&](const KvTile<NJ>& T, int k) {
+      const int t0 = first + STEP * k;
+      if (t0 + 32 > end_t || t0 + 32 > see0 || T.bad)
+        work(T, t0, std::true_type{});
+      else
+        work(T, t0, std::false_type{});
+    };
+    // this wave's tiles, the next one loaded meanwhile
+    const int count = end_t > first ? (end_t - first + STEP - 1) / STEP : 0;
+    if (count > 0) {
+      KvTile<NJ> T0, T1;
+      load(T0, 0);
+      for (int k = 0;;) {
+        if (k + 1 < count) load(T1, k + 1);
+        turn(T0, k);
+        if (++k >= count) break;
+        if (k + 1 < count) load(T0, k + 1);
+        turn(T1, k);
+        if (++k >= count) break;
       }
     }
-
-    // the waves' parts to LDS
 #pragma unroll
     for (int i = 0; i < MQ; ++i) {
       l[i] += __shfl_xor(l[i], 16);
       l[i] += __shfl_xor(l[i], 32);
       zs[i] += __shfl_xor(zs[i], 16);
       zs[i] += __shfl_xor(zs[i], 32);
+    }
+    // channel of block d of this lane
+    auto channel = [&](int d) { return DIM == 128 ? 8 * n + d : 8 * (n & 7) + 4 * (n >> 3) + d; };
+
+    if constexpr (BY_ROWS) {
+#pragma unroll
+      for (int i = 0; i < MQ; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = row0 + 16 * i + 4 * g4 + r;
+          const float z = __shfl(zs[i], 4 * g4 + r), sum = __shfl(l[i], 4 * g4 + r);
+          const float mm = __shfl(m[i], 4 * g4 + r);
+          const bool whole = A.splits == 1;
+          const float f = !whole ? sigma : sum == 0.f ? 0.f : sigma / sum;  // (sees nothing: zeros)
+          float o[ND];
+#pragma unroll
+          for (int d = 0; d < ND; ++d) o[d] = f * (acc[i][d][r] * (d & 1 ? 0x1p20f : 0x1p24f) - z);
+          if (whole && A.rotate) {
+            hadamard_reg<ND>(o);
+            turn16<ND>(o, n);
+            const float norm = DIM == 128 ? 0.08838834764831845f : 0.125f;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) o[d] *= norm;
+          }
+          if (row >= nrows) continue;
+          const int64_t tok = q0 + row / G;
+          const int head = h * G + row % G;
+          if (whole) {
+            uint16_t* out = A.out + tok * A.ldo + int64_t(head) * DIM + channel(0);
+#pragma unroll
+            for (int d = 0; d < ND; ++d) out[d] = f32_bf16(o[d]);
+          } else {
+            const int64_t at = (int64_t(split) * A.n_tokens + tok) * A.n_heads + head;
+#pragma unroll
+            for (int d = 0; d < ND; d += 4)
+              *reinterpret_cast<f32x4_t*>(A.part + at * DIM + channel(d)) =
+                  f32x4_t{o[d], o[d + 1], o[d + 2], o[d + 3]};
+            if (n == 0) A.ml[2 * at] = mm, A.ml[2 * at + 1] = sum;
+          }
+        }
+      continue;
+    }
+    // the waves' parts to LDS
+#pragma unroll
+    for (int i = 0; i < MQ; ++i) {
       float* o = sm + (wave * ROWS + 16 * i) * LD;
       if (g4 == 0) {
         sml[(wave * ROWS + 16 * i + n) * 2] = m[i];
@@ -499,11 +583,9 @@ __global__ __launch_bounds__(256) void cache_attention(AttnArgs A) {
       for (int r = 0; r < 4; ++r) {
         const float z = __shfl(zs[i], 4 * g4 + r);
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          const float v = sigma * (acc[i][d][r] * (d & 1 ? 0x1p20f : 0x1p24f) - z);
-          const int ch = DIM == 128 ? 8 * n + d : 8 * (n & 7) + 4 * (n >> 3) + d;
-          o[(4 * g4 + r) * LD + ch] = v;
-        }
+        for (int d = 0; d < ND; ++d)
+          o[(4 * g4 + r) * LD + channel(d)] =
+              sigma * (acc[i][d][r] * (d & 1 ? 0x1p20f : 0x1p24f) - z);
       }
     }
     __syncthreads();
@@ -572,12 +654,12 @@ int64_t split_rows(int64_t rows) {
   return rows * MAX_SPLITS < SPLIT_ROWS + rows ? rows * MAX_SPLITS : SPLIT_ROWS + rows;
 }
 
-template <int DIM, int MQ>
+template <int DIM, int MQ, bool BY_ROWS>
 int launch_attention(const AttnArgs& a, int64_t n_seqs, hipStream_t s) {
-  const size_t lds = size_t(4) * 16 * MQ * (DIM + 4 + 2) * sizeof(float);
+  const size_t lds = BY_ROWS ? 0 : size_t(4) * 16 * MQ * (DIM + 4 + 2) * sizeof(float);
   const dim3 grid(static_cast<unsigned>(a.tiles * a.splits), static_cast<unsigned>(a.n_kv),
                   static_cast<unsigned>(n_seqs));
-  KQ_TRY(launch("cache_attention", cache_attention<DIM, MQ>, grid, dim3(256), lds, s, a));
+  KQ_TRY(launch("cache_attention", cache_attention<DIM, MQ, BY_ROWS>, grid, dim3(256), lds, s, a));
   if (a.splits == 1) return KRONQ_OK;
   return launch("attention_join", attention_join<DIM>,
                 dim3(static_cast<unsigned>(cdiv(a.n_tokens * a.n_heads, 4))), dim3(256), 0, s, a,
@@ -616,11 +698,15 @@ int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {
   a.table = j.table, a.ldt = j.ldt, a.table_pages = int(j.table_pages), a.lengths = j.lengths;
   a.starts = j.starts, a.scale = j.scale * 1.4426950408889634f, a.rotate = j.rotate;
   a.out = static_cast<uint16_t*>(j.out), a.ldo = j.ldo;
-  const int64_t rows = j.max_new * a.group;  // of a sequence and kv head
-  const int mq = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  a.tiles = int(cdiv(rows, 16 * mq));
+  // Up to 64 rows of a sequence and kv head share their tokens out to the waves (two tiles of 32 rows
+  // from 33 on); more are walked by 128 rows a workgroup, which read the tokens once for all of them.
+  const int64_t rows = j.max_new * a.group;
+  const bool by_rows = rows > 64;
+  const int mq = rows <= 16 ? 1 : 2;
+  a.tiles = int(cdiv(rows, by_rows ? 64 * mq : 16 * mq));
+  // enough workgroups for sequences of different lengths to even out, of 256 tokens each at least
   const int64_t wgs = a.tiles * j.n_kv * j.n_seqs, all = j.n_tokens * j.n_heads;
-  int64_t splits = cdiv(1024, wgs);
+  int64_t splits = cdiv(by_rows ? 512 : 3072, wgs);
   const int64_t useful = cdiv(j.table_pages * j.page, 256);
   splits = splits < useful ? splits : useful;
   splits = splits < MAX_SPLITS ? splits : MAX_SPLITS;
@@ -631,12 +717,12 @@ int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {
   a.part = cv.take<float>(cap * size_t(j.dim));
   a.ml = cv.take<float>(cap * 2);
   if (j.dim == 128)
-    return mq == 1   ? launch_attention<128, 1>(a, j.n_seqs, s)
-           : mq == 2 ? launch_attention<128, 2>(a, j.n_seqs, s)
-                     : launch_attention<128, 4>(a, j.n_seqs, s);
-  return mq == 1   ? launch_attention<64, 1>(a, j.n_seqs, s)
-         : mq == 2 ? launch_attention<64, 2>(a, j.n_seqs, s)
-                   : launch_attention<64, 4>(a, j.n_seqs, s);
+    return mq == 1   ? launch_attention<128, 1, false>(a, j.n_seqs, s)
+           : by_rows ? launch_attention<128, 2, true>(a, j.n_seqs, s)
+                     : launch_attention<128, 2, false>(a, j.n_seqs, s);
+  return mq == 1   ? launch_attention<64, 1, false>(a, j.n_seqs, s)
+         : by_rows ? launch_attention<64, 2, true>(a, j.n_seqs, s)
+                   : launch_attention<64, 2, false>(a, j.n_seqs, s);
 }
 
 }  // namespace kq
