@@ -219,12 +219,19 @@ __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
                                                 __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
 }
 
-// what a wave loads of 32 tokens: codes and parameters of both halves of 16
-template <int NJ>
-struct KvTile {
-  uint32_t k[2][NJ], v[2][4], kp[2][4], vp[2][4];
-  int bad;  // halves on pages that do not exist
-};
+#define KQ_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+template <int N>
+__device__ __forceinline__ void wait_vm() {  // s_waitcnt vmcnt(N), the other counters free
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+
+// What a wave keeps in LDS of 32 tokens, in two halves of 16: for each lane the words of its key row
+// and of its value channels as it wants them (16 bytes a lane and load, one behind another), and the
+// parameters of 16 keys and 16 values. The loads go straight there, DEPTH tiles ahead: registers for
+// a second tile left one wave less per SIMD and a single tile of each wave on its way (156 us where it
+// takes XXX, 48 sequences of up to 16384 tokens).
+constexpr int DEPTH = 4;
+constexpr int tile_words(int dim) { return 2 * (64 * (dim / 32) + 256 + 64); }
 
 template <int DIM, int MQ, bool BY_ROWS>
 __global__ __launch_bounds__(256, MQ == 1 ? 2 : 2) void cache_attention(AttnArgs A) {
@@ -233,7 +240,9 @@ __global__ __launch_bounds__(256, MQ == 1 ? 2 : 2) void cache_attention(AttnArgs
   constexpr int WPR = DIM / 8;       // words per row
   constexpr int ROWS = 16 * MQ, TILE = BY_ROWS ? 4 * ROWS : ROWS, LD = DIM + 4;
   constexpr int STEP = BY_ROWS ? 32 : 128;  // tokens from one of a wave's tiles to the next
-  extern __shared__ __attribute__((aligned(16))) float sm[];  // [wave][row][LD], [wave][row][2]
+  constexpr int TW = tile_words(DIM), HALF = TW / 2, AT_V = 64 * NJ, AT_P = AT_V + 256;
+  // the waves' tiles [wave][DEPTH][TW]; at the end [wave][row][LD] and [wave][row][2]
+  extern __shared__ __attribute__((aligned(16))) float sm[];
   float* sml = sm + 4 * ROWS * LD;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -333,47 +342,71 @@ __global__ __launch_bounds__(256, MQ == 1 ? 2 : 2) void cache_attention(AttnArgs
     for (int i = 0; i < MQ; ++i) m[i] = -1e30f, l[i] = 0.f, zs[i] = 0.f;
 
     // The pages of this wave's next 32 tiles, one of their halves of 16 a lane: read one by one, each
-    // tile would wait for its page before it could ask for its codes.
+    // tile would wait for its page before it could ask for its codes. Tokens past the end: the last
+    // ones again, masked below.
     const int first = beg_t + (BY_ROWS ? 0 : 32 * wave);
     int pages = 0, k0 = -32;
-    // past the end: the last tokens again, masked below
-    const unsigned at_k = n * WPR + g4 * NJ, at_v = (g4 * WPR + (n & (WPR - 1))) * 4, at_p = 4 * g4;
+    const unsigned at_k = (n * WPR + g4 * NJ) * 4, at_v = (g4 * WPR + (n & (WPR - 1))) * 16;
+    const unsigned at_p = (n + ((lane & 16) << A.page_log >> 4)) * 4;  // keys, then values
+    uint32_t* const ring = reinterpret_cast<uint32_t*>(sm) + wave * DEPTH * TW;
     auto token = [&](int t) { return t < end ? t : (end - 1) & ~15; };
-    auto load = [&](KvTile<NJ>& T, int k) {  // this wave's tile k
+    const int count = end_t > first ? (end_t - first + STEP - 1) / STEP : 0;
+    unsigned bad = 0;  // two bits a tile under way: halves on pages that do not exist
+    auto load = [&](int k) {  // this wave's tile k (past the end the last one, to a place of its own)
+      const int place = k & (DEPTH - 1);
+      k = k < count ? k : count - 1;
       if (k >= k0 + 32) {
         k0 = k;
         pages = table[token(first + STEP * (k + (lane >> 1)) + 16 * (lane & 1)) >> A.page_log];
       }
-      T.bad = 0;
+      uint32_t* const to = ring + place * TW;
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
         const int t = token(first + STEP * k + 16 * f);
         int p = __builtin_amdgcn_readlane(pages, 2 * (k - k0) + f);
-        if (p < 0 || p >= A.n_pages) p = 0, T.bad |= 1 << f;
-        // (uniform bases and the lane's 32-bit offsets: no 64-bit address is held per lane)
+        const unsigned bit = 1u << (2 * place + f);
+        bad &= ~bit;
+        if (p < 0 || p >= A.n_pages) p = 0, bad |= bit;
         const int64_t slot = (((int64_t(p) * A.n_kv + h) * 2) << A.page_log) + (t & page_mask);
-        const uint32_t* const kc = A.codes + slot * WPR + at_k;
-        const uint32_t* const vc = A.codes + (slot + (1 << A.page_log)) * WPR + at_v;
-        const uint32_t* const pp = A.params + slot + at_p;
+        const auto codes = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint32_t*>(A.codes + slot * WPR), 0, 0x7FFFFFFF, 0x00027000);
+        const auto params = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint32_t*>(A.params + slot), 0, 0x7FFFFFFF, 0x00027000);
+        uint32_t* const half = to + f * HALF;
         if constexpr (NJ == 4) {
-          const uint4 w = *reinterpret_cast<const uint4*>(kc);
-          T.k[f][0] = w.x, T.k[f][1] = w.y, T.k[f][2] = w.z, T.k[f][3] = w.w;
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(codes, KQ_LDS(half), 16, at_k, 0, 0, 0);
         } else {
-          const uint2 w = *reinterpret_cast<const uint2*>(kc);
-          T.k[f][0] = w.x, T.k[f][1] = w.y;
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(codes, KQ_LDS(half), 4, at_k, 0, 0, 0);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(codes, KQ_LDS(half + 64), 4, at_k, 4, 0, 0);
         }
-        const uint4 v = *reinterpret_cast<const uint4*>(vc);
-        T.v[f][0] = v.x, T.v[f][1] = v.y, T.v[f][2] = v.z, T.v[f][3] = v.w;
-        const uint4 a = *reinterpret_cast<const uint4*>(pp);
-        T.kp[f][0] = a.x, T.kp[f][1] = a.y, T.kp[f][2] = a.z, T.kp[f][3] = a.w;
-        const uint4 c = *reinterpret_cast<const uint4*>(pp + (1 << A.page_log));
-        T.vp[f][0] = c.x, T.vp[f][1] = c.y, T.vp[f][2] = c.z, T.vp[f][3] = c.w;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(codes, KQ_LDS(half + AT_V), 16, at_v,
+                                                 (WPR * 4) << A.page_log, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(params, KQ_LDS(half + AT_P), 4, at_p, 0, 0, 0);
       }
     };
+    constexpr int LOADS = 2 * (NJ == 4 ? 3 : 4);  // of a tile
 
     // CUT: some of the tokens do not count, or not for every row
-    auto work = [&](const KvTile<NJ>& T, int t0, auto cut_c) {
+    auto work = [&](int k, int t0, unsigned off, auto cut_c) {
       constexpr bool CUT = decltype(cut_c)::value;
+      const uint32_t* const tile = ring + (k & (DEPTH - 1)) * TW;
+      struct {
+        uint32_t k[2][NJ], v[2][4], kp[2][4], vp[2][4];
+      } T;
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const uint32_t* const half = tile + f * HALF;
+        if constexpr (NJ == 4) {
+          const u32x4_t w = *reinterpret_cast<const u32x4_t*>(half + 4 * lane);
+          T.k[f][0] = w[0], T.k[f][1] = w[1], T.k[f][2] = w[2], T.k[f][3] = w[3];
+        } else {
+          T.k[f][0] = half[lane], T.k[f][1] = half[lane + 64];
+        }
+        const u32x4_t a = *reinterpret_cast<const u32x4_t*>(half + AT_P + 4 * g4);
+        const u32x4_t c = *reinterpret_cast<const u32x4_t*>(half + AT_P + 16 + 4 * g4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) T.kp[f][r] = a[r], T.vp[f][r] = c[r];
+      }
       f32x4_t s[MQ][2] = {};
 #pragma unroll
       for (int f = 0; f < 2; ++f)
@@ -387,7 +420,7 @@ __global__ __launch_bounds__(256, MQ == 1 ? 2 : 2) void cache_attention(AttnArgs
       __builtin_amdgcn_sched_barrier(0);  // (else all codes are spread ahead, and registers spill)
       // does this lane's token 16 f + 4 g4 + r count at all
       auto counts = [&](int f, int r) {
-        return !CUT || (t0 + 16 * f + 4 * g4 + r < end_t && !(T.bad >> f & 1));
+        return !CUT || (t0 + 16 * f + 4 * g4 + r < end_t && !(off >> f & 1));
       };
       // its value scale (what stands in a place that does not count is nothing)
       auto value_scale = [&](int f, int r) {
@@ -443,6 +476,12 @@ __global__ __launch_bounds__(256, MQ == 1 ? 2 : 2) void cache_attention(AttnArgs
         }
       }
       __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const u32x4_t w = *reinterpret_cast<const u32x4_t*>(tile + f * HALF + AT_V + 4 * lane);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) T.v[f][r] = w[r];
+      }
       u32x4_t pf[MQ];
 #pragma unroll
       for (int f = 0; f < 2; ++f)
@@ -502,26 +541,21 @@ __global__ __launch_bounds__(256, MQ == 1 ? 2 : 2) void cache_attention(AttnArgs
       }
     };
 
-    auto turn = [&](const KvTile<NJ>& T, int k) {
-      const int t0 = first + STEP * k;
-      if (t0 + 32 > end_t || t0 + 32 > see0 || T.bad)
-        work(T, t0, std::true_type{});
-      else
-        work(T, t0, std::false_type{});
-    };
-    // this wave's tiles, the next one loaded meanwhile
-    const int count = end_t > first ? (end_t - first + STEP - 1) / STEP : 0;
+    // this wave's tiles
     if (count > 0) {
-      KvTile<NJ> T0, T1;
-      load(T0, 0);
-      for (int k = 0;;) {
-        if (k + 1 < count) load(T1, k + 1);
-        turn(T0, k);
-        if (++k >= count) break;
-        if (k + 1 < count) load(T0, k + 1);
-        turn(T1, k);
-        if (++k >= count) break;
+      for (int k = 0; k < DEPTH - 1; ++k) load(k);
+      for (int k = 0; k < count; ++k) {
+        load(k + DEPTH - 1);  // (to the place of the tile before this one, which has been read)
+        wait_vm<(DEPTH - 1) * LOADS>();
+        __builtin_amdgcn_sched_barrier(0);
+        const int t0 = first + STEP * k;
+        const unsigned off = bad >> (2 * (k & (DEPTH - 1))) & 3;
+        if (t0 + 32 > end_t || t0 + 32 > see0 || off)
+          work(k, t0, off, std::true_type{});
+        else
+          work(k, t0, off, std::false_type{});
       }
+      wait_vm<0>();  // (loads past the end)
     }
 #pragma unroll
     for (int i = 0; i < MQ; ++i) {
@@ -571,7 +605,8 @@ __global__ __launch_bounds__(256, MQ == 1 ? 2 : 2) void cache_attention(AttnArgs
         }
       continue;
     }
-    // the waves' parts to LDS
+    // the waves' parts to LDS, where their tiles were
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < MQ; ++i) {
       float* o = sm + (wave * ROWS + 16 * i) * LD;
@@ -656,7 +691,9 @@ int64_t split_rows(int64_t rows) {
 
 template <int DIM, int MQ, bool BY_ROWS>
 int launch_attention(const AttnArgs& a, int64_t n_seqs, hipStream_t s) {
-  const size_t lds = BY_ROWS ? 0 : size_t(4) * 16 * MQ * (DIM + 4 + 2) * sizeof(float);
+  const size_t tiles = size_t(4) * DEPTH * tile_words(DIM) * 4;
+  const size_t ends = BY_ROWS ? 0 : size_t(4) * 16 * MQ * (DIM + 4 + 2) * sizeof(float);
+  const size_t lds = tiles > ends ? tiles : ends;
   const dim3 grid(static_cast<unsigned>(a.tiles * a.splits), static_cast<unsigned>(a.n_kv),
                   static_cast<unsigned>(n_seqs));
   KQ_TRY(launch("cache_attention", cache_attention<DIM, MQ, BY_ROWS>, grid, dim3(256), lds, s, a));
