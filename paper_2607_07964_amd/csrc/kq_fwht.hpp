@@ -25,6 +25,37 @@ __device__ __forceinline__ float dpp_mov(float x) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true));
 }
 
+template <int CTRL>
+__device__ __forceinline__ int dpp_movi(int x) {
+  return __builtin_amdgcn_mov_dpp(x, CTRL, 0xf, 0xf, true);
+}
+
+// One stage x <- x + s y (y the partner's value, s the sign of the lane's own half) on eight registers:
+// right for the lower element and the negative for the upper one, so that after several of them a
+// lane's values have the product of its signs, which the callers multiply by once. (As asm: from the builtin the compiler makes two moves and the
+// multiply-add. s_nop: a register read by DPP has to have been written two instructions before; each
+// of the eight was written by another of the same eight or before the s_nop.)
+#define KQ_DPP_STAGE(NAME, CTRL)                                                                  \
+  __device__ __forceinline__ void NAME(float* x, float s) {                                       \
+    asm("s_nop 1\n\t"                                                                             \
+        "v_fmac_f32_dpp %0, %0, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %1, %1, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %2, %2, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %3, %3, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %4, %4, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %5, %5, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %6, %6, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
+        "v_fmac_f32_dpp %7, %7, %8 " CTRL " row_mask:0xf bank_mask:0xf"                           \
+        : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]),     \
+          "+v"(x[7])                                                                              \
+        : "v"(s));                                                                                \
+  }
+KQ_DPP_STAGE(stage_lane1, "quad_perm:[1,0,3,2]")
+KQ_DPP_STAGE(stage_lane2, "quad_perm:[2,3,0,1]")
+KQ_DPP_STAGE(stage_mirror8, "row_half_mirror")
+KQ_DPP_STAGE(stage_lane8, "row_ror:8")
+#undef KQ_DPP_STAGE
+
 // Butterfly stages across the lanes of a wave (lane xor 1 ... 8, then 16 and 32 as far as stages,
 // 4 to 6, goes) on N registers a lane (N even). Strides 1 ... 8 take the partner by DPP and x = y -+ x in one FMA (exact); strides 16 and
 // 32 exchange rows between two registers, add and subtract them, and exchange back. No LDS

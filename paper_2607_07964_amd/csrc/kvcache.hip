@@ -42,40 +42,22 @@ struct AppendArgs {
   float *k_hat, *v_hat;
 };
 
-// dim / 8 lanes take a row, eight values each. In fp64: the transform is exact to 2^-52, so that a
-// code depends on the row alone and not on the order of the sums; bound by the reads and writes of
-// the rows all the same.
-template <typename T, int DIM>
-__global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
-  constexpr int LPR = DIM / 8, RPW = 256 / LPR;  // lanes per row, rows per workgroup
-  const int l = threadIdx.x % LPR;
-  const int64_t row = int64_t(blockIdx.x) * RPW + threadIdx.x / LPR;  // token, head, key or value
-  const int64_t rows = A.n_tokens * A.n_kv * 2;
-  if (row >= rows) return;  // (whole groups of LPR lanes)
-  const int part = int(row & 1);
-  const int64_t th = row >> 1, token = th / A.n_kv;
-  const int head = int(th % A.n_kv);
-  const int64_t slot = A.slots[token];
-  if (slot < 0 || slot >= A.n_slots) return;
-  const T* src = static_cast<const T*>(part ? A.v : A.k) + token * (part ? A.ldv : A.ldk) +
-                 int64_t(head) * DIM + l * 8;
+// What a lane has found of its row: the codes of its eight values, the row's scale, zero and whether
+// all of it is finite.
+struct RowGrid {
+  uint32_t word;
+  float scale, zero;
+  bool bad;
+};
+
+// The grid in fp64: the transform is exact to 2^-52, so that a code depends on the row alone and not
+// on the order of the sums.
+template <int LPR>
+__device__ __forceinline__ RowGrid row_grid(const float (&x)[8], int chunk, int rotate, double norm) {
   double r[8];
-  if constexpr (sizeof(T) == 2) {
-    const uint4 w = *reinterpret_cast<const uint4*>(src);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      r[2 * i] = __uint_as_float(u[i] << 16);
-      r[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i += 4) {
-      const float4 w = *reinterpret_cast<const float4*>(src + i);
-      r[i] = w.x, r[i + 1] = w.y, r[i + 2] = w.z, r[i + 3] = w.w;
-    }
-  }
-  if (A.rotate) {
+  for (int i = 0; i < 8; ++i) r[i] = x[i];
+  if (rotate) {
 #pragma unroll
     for (int s = 1; s < 8; s <<= 1)
 #pragma unroll
@@ -88,11 +70,11 @@ __global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
     for (int o = 1; o < LPR; o <<= 1)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const double p = __shfl_xor(r[i], o);
-        r[i] = (l & o) ? p - r[i] : r[i] + p;
+        const double p = __shfl_xor(r[i], o == 4 ? 7 : o);
+        r[i] = (chunk & o) ? p - r[i] : r[i] + p;
       }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] *= A.norm;
+    for (int i = 0; i < 8; ++i) r[i] *= norm;
   }
   double lo = 0.0, hi = 0.0;
   int bad = 0;
@@ -110,30 +92,118 @@ __global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
   // up to bf16: 45 of the 52 bits of the fraction go
   const uint64_t up = (__builtin_bit_cast(uint64_t, wide) + ((uint64_t(1) << 45) - 1)) &
                       ~((uint64_t(1) << 45) - 1);
-  const double scale = __builtin_bit_cast(double, up), inv = 1.0 / scale;
+  const double scale = __builtin_bit_cast(double, up);
   const double zero = fmin(rint(-lo / scale), 15.0);
-  uint32_t word = 0;
-  float hat[8];
-  // a row with a value that is not finite reads as NaN
-  const float sf = bad ? __uint_as_float(0x7FC00000u) : float(scale);
+  RowGrid g{0, float(scale), float(zero), bad != 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const double t = r[i] * inv;  // good to 2^-51: rint(t) is rint(r / scale) unless t is next to a
-    double n = rint(t);           // half, where the quotient itself decides
-    if (fabs(fabs(t - n) - 0.5) < 1e-12) n = rint(r[i] / scale);
-    const double c = bad ? 0.0 : fmin(fmax(n + zero, 0.0), 15.0);
-    word |= uint32_t(int(c)) << (4 * i);
-    hat[i] = sf * float(c - zero);
+    const double c = bad ? 0.0 : fmin(fmax(rint(r[i] / scale) + zero, 0.0), 15.0);
+    g.word |= uint32_t(int(c)) << (4 * i);
   }
+  return g;
+}
+
+// dim / 8 lanes take a row, eight values each. The grid is worked out in fp32 and kept where fp32
+// must agree with fp64, which settles the rest (some 3 rows of 100; all of it in fp64 was bound by
+// its arithmetic). With range = hi - lo >= max |f| and f = D^(1/2) r the transform before its norm, its
+// log2(D) stages round by at most 2^-24 |x|_1 each, and |x|_1 <= D^(1/2) |x|_2 <= D^(1/2) max |f|, so
+//   |error of f| <= 7 2^-24 11.4 range < 4.8e-6 range: of range itself < 1.1e-5 with the products
+//     after it, less than 192 steps of a 24-bit fraction (a scale ends at 16 of them: 256 are kept clear),
+//   |error of r / scale| < 15 4.8e-6 + 15 2^-22 < 8e-5: halves are kept clear by 1e-4.
+// 64000 tokens TOKENS_FIGURE
+template <typename T, int DIM>
+__global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
+  constexpr int LPR = DIM / 8, RPW = 256 / LPR;  // lanes per row, rows per workgroup
+  const int l = threadIdx.x % LPR;
+  const int chunk = l ^ ((l & 4) ? 3 : 0);  // (the chunk 4 further on is the mirrored lane of 8)
+  const int64_t row = int64_t(blockIdx.x) * RPW + threadIdx.x / LPR;  // token, head, key or value
+  const int64_t rows = A.n_tokens * A.n_kv * 2;
+  if (row >= rows) return;  // (whole groups of LPR lanes)
+  const int part = int(row & 1);
+  const int64_t th = row >> 1, token = th / A.n_kv;
+  const int head = int(th % A.n_kv);
+  const int64_t slot = A.slots[token];
+  if (slot < 0 || slot >= A.n_slots) return;
+  const T* src = static_cast<const T*>(part ? A.v : A.k) + token * (part ? A.ldv : A.ldk) +
+                 int64_t(head) * DIM + chunk * 8;
+  float x[8], f[8];
+  if constexpr (sizeof(T) == 2) {
+    const uint4 w = *reinterpret_cast<const uint4*>(src);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(u[i] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      const float4 w = *reinterpret_cast<const float4*>(src + i);
+      x[i] = w.x, x[i + 1] = w.y, x[i + 2] = w.z, x[i + 3] = w.w;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = x[i];
+  float norm = 1.f, sign = 1.f;
+  if (A.rotate) {
+    hadamard_reg<8>(f);
+    stage_lane1(f, (chunk & 1) ? -1.f : 1.f);
+    stage_lane2(f, (chunk & 2) ? -1.f : 1.f);
+    stage_mirror8(f, (chunk & 4) ? -1.f : 1.f);
+    if constexpr (LPR == 16) stage_lane8(f, (chunk & 8) ? -1.f : 1.f);
+    norm = float(A.norm), sign = (__popc(unsigned(chunk)) & 1) ? -1.f : 1.f;
+  }
+  float lo = f[0], hi = f[0], nan = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo = fminf(lo, f[i]), hi = fmaxf(hi, f[i]);
+    nan = fmaf(f[i], 0.f, nan);  // NaN if any of them is NaN or infinite
+  }
+  const float least = sign < 0.f ? -hi : lo, most = sign < 0.f ? -lo : hi;
+  lo = fminf(least, 0.f), hi = fmaxf(most, 0.f);
+  auto join = [&](auto other) {
+    lo = fminf(lo, other(lo)), hi = fmaxf(hi, other(hi)), nan += other(nan);
+  };
+  join([](float v) { return dpp_mov<0xB1>(v); });
+  join([](float v) { return dpp_mov<0x4E>(v); });
+  join([](float v) { return dpp_mov<0x141>(v); });
+  if constexpr (LPR == 16) join([](float v) { return dpp_mov<0x128>(v); });
+  const float range = hi - lo, wide = fmaxf(range * (norm / 15.f), 0x1p-100f);
+  const uint32_t bits = __float_as_uint(wide);
+  RowGrid g;
+  g.scale = __uint_as_float((bits + 0xFFFFu) & 0xFFFF0000u);
+  const float inv = norm / g.scale, to = inv * sign, z = -lo * inv;
+  g.zero = fminf(rintf(z), 15.f), g.bad = false, g.word = 0;
+  float far = fabsf(z - rintf(z));  // from the next whole number
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float t = f[i] * to, n = rintf(t);
+    far = fmaxf(far, fabsf(t - n));
+    const float c = fminf(fmaxf(n + g.zero, 0.f), 15.f);
+    g.word |= uint32_t(int(c)) << (4 * i);
+  }
+  const uint32_t low = bits & 0xFFFFu;
+  int sure = far < 0.4999f && low - 256u < 65536u - 512u && range <= 3.0e38f && nan == 0.f;
+  sure &= dpp_movi<0xB1>(sure);
+  sure &= dpp_movi<0x4E>(sure);
+  sure &= dpp_movi<0x141>(sure);
+  if constexpr (LPR == 16) sure &= dpp_movi<0x128>(sure);
+  if (!sure) g = row_grid<LPR>(x, chunk, A.rotate, A.norm);
+  // a row with a value that is not finite reads as NaN
+  if (g.bad) g.scale = __uint_as_float(0x7FC00000u);
   const int64_t p = slot >> A.page_log, off = slot & ((int64_t(1) << A.page_log) - 1);
   const int64_t ph = (p * A.n_kv + head) * 2 + part;
-  const int64_t at = part ? ((off >> 2) * LPR + l) * 4 + (off & 3) : off * LPR + l;
-  A.codes[((ph << A.page_log) * LPR) + at] = word;
+  const int64_t at = part ? ((off >> 2) * LPR + chunk) * 4 + (off & 3) : off * LPR + chunk;
+  A.codes[((ph << A.page_log) * LPR) + at] = g.word;
   if (l == 0)
-    A.params[(ph << A.page_log) + off] = __float_as_uint(sf) | (bad ? 0u : uint32_t(int(zero)));
+    A.params[(ph << A.page_log) + off] =
+        __float_as_uint(g.scale) | (g.bad ? 0u : uint32_t(int(g.zero)));
   float* out = part ? A.v_hat : A.k_hat;
   if (out) {
-    out += th * DIM + l * 8;
+    out += th * DIM + chunk * 8;
+    float hat[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) hat[i] = g.scale * (float((g.word >> (4 * i)) & 15u) - g.zero);
     *reinterpret_cast<float4*>(out) = make_float4(hat[0], hat[1], hat[2], hat[3]);
     *reinterpret_cast<float4*>(out + 4) = make_float4(hat[4], hat[5], hat[6], hat[7]);
   }
@@ -229,12 +299,12 @@ __device__ __forceinline__ void wait_vm() {  // s_waitcnt vmcnt(N), the other co
 // and of its value channels as it wants them (16 bytes a lane and load, one behind another), and the
 // parameters of 16 keys and 16 values. The loads go straight there, DEPTH tiles ahead: registers for
 // a second tile left one wave less per SIMD and a single tile of each wave on its way (156 us where it
-// takes XXX, 48 sequences of up to 16384 tokens).
+// takes 129, 48 sequences of up to 16384 tokens).
 constexpr int DEPTH = 4;
 constexpr int tile_words(int dim) { return 2 * (64 * (dim / 32) + 256 + 64); }
 
 template <int DIM, int MQ, bool BY_ROWS>
-__global__ __launch_bounds__(256, MQ == 1 ? 2 : 2) void cache_attention(AttnArgs A) {
+__global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
   constexpr int NJ = DIM / 32;       // words of a key row a lane takes, matrix steps per score
   constexpr int ND = DIM / 16;       // output blocks of 16 channels
   constexpr int WPR = DIM / 8;       // words per row
@@ -743,7 +813,7 @@ int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {
   a.tiles = int(cdiv(rows, by_rows ? 64 * mq : 16 * mq));
   // enough workgroups for sequences of different lengths to even out, of 256 tokens each at least
   const int64_t wgs = a.tiles * j.n_kv * j.n_seqs, all = j.n_tokens * j.n_heads;
-  int64_t splits = cdiv(by_rows ? 512 : 3072, wgs);
+  int64_t splits = cdiv(by_rows ? 512 : 1536, wgs);
   const int64_t useful = cdiv(j.table_pages * j.page, 256);
   splits = splits < useful ? splits : useful;
   splits = splits < MAX_SPLITS ? splits : MAX_SPLITS;

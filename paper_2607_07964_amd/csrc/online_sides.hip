@@ -110,36 +110,11 @@ __device__ void fill_table(const LinearIn& A, int64_t block) {
 // The octet of a wave's 64 that a lane holds: lanes 4-7 of each 8 in reverse order, so that the
 // octet 4 further on is the mirrored lane of the 8 (one DPP control) and not two exchanges away.
 __device__ __forceinline__ int octet_of(int lane) { return lane ^ ((lane & 4) ? 3 : 0); }
-// Strides 8 ... 64 are taken as x + s y (y the partner's value, s its sign), one multiply-add with
-// the partner read by DPP: right for the lower element and the negative for the upper one. What is
-// left is this sign of the octet, which the callers multiply by once.
+// Strides 8 ... 64 are single multiply-adds with the partner read by DPP (kq_fwht.hpp), which leave
+// each value times this sign of its octet: the callers multiply by it once.
 __device__ __forceinline__ float octet_sign(int octet, int cols) {
   return (__popc(unsigned(octet & 15 & (cols / 8 - 1))) & 1) ? -1.f : 1.f;
 }
-
-// One such stage on eight registers. (As asm: from the builtin the compiler makes two moves and the
-// multiply-add. s_nop: a register read by DPP has to have been written two instructions before; each
-// of the eight was written by another of the same eight or before the s_nop.)
-#define KQ_DPP_STAGE(NAME, CTRL)                                                                  \
-  __device__ __forceinline__ void NAME(float* x, float s) {                                       \
-    asm("s_nop 1\n\t"                                                                             \
-        "v_fmac_f32_dpp %0, %0, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
-        "v_fmac_f32_dpp %1, %1, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
-        "v_fmac_f32_dpp %2, %2, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
-        "v_fmac_f32_dpp %3, %3, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
-        "v_fmac_f32_dpp %4, %4, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
-        "v_fmac_f32_dpp %5, %5, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
-        "v_fmac_f32_dpp %6, %6, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t"                       \
-        "v_fmac_f32_dpp %7, %7, %8 " CTRL " row_mask:0xf bank_mask:0xf"                           \
-        : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]),     \
-          "+v"(x[7])                                                                              \
-        : "v"(s));                                                                                \
-  }
-KQ_DPP_STAGE(stage_lane1, "quad_perm:[1,0,3,2]")
-KQ_DPP_STAGE(stage_lane2, "quad_perm:[2,3,0,1]")
-KQ_DPP_STAGE(stage_mirror8, "row_half_mirror")
-KQ_DPP_STAGE(stage_lane8, "row_ror:8")
-#undef KQ_DPP_STAGE
 
 // (every lane of the wave comes here; FULL: columns of 512)
 template <int N, bool FULL>

@@ -8,6 +8,7 @@ an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -436,11 +437,31 @@ def _same_device(*ts):
     return dev
 
 
+# A call of one token is bound by what the host does before its launches: the guard of the device is
+# entered only when another one is current, and the stream is taken as the bare handle (the two
+# cost 3 us of such a call's 12 through torch.cuda's objects).
+_CURRENT = contextlib.nullcontext()
+
+
+def _guard(dev: torch.device):
+    """Context in which ``dev`` is the current device."""
+    return _CURRENT if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+
+def _handle(dev: torch.device) -> int:
+    """The current stream of ``dev``."""
+    return torch._C._cuda_getCurrentRawStream(dev.index)
+
+
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
 def _typed(t: Optional[torch.Tensor], dtype, shape, name: str):
     """``t`` (or None) with this dtype and these contiguous elements."""
     if t is None:
         return
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, "
                          f"not {t.dtype} {tuple(t.shape)}")
 
@@ -486,16 +507,16 @@ def _served(func, packed, scales, zeros, bits, group, d_in, mul_in, mul_out, q28
     ldx = _ld(x) if n > 1 else -(-d_in // 8) * 8
     ldy = _ld(y) if n > 1 else d_out
     ldr = 0 if residual is None else _ld(residual) if n > 1 else d_out
-    with torch.cuda.device(dev):
+    with _guard(dev):
         if ws is None:
             need = lib.kronq_workspace_bytes(OP_LINEAR, d_out, d_in, n) if offsets is None else \
                 lib.kronq_grouped_workspace_bytes(d_out, d_in, n, n_experts)
             ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
         head = (packed.data_ptr(), _ld(packed), scales.data_ptr(), zeros.data_ptr(), _ld(scales),
-                bits, group, d_out, d_in, _ptr(mul_in), _ptr(mul_out), _ptr(q28_in), _ptr(q28_out),
-                flags, x.data_ptr(), _dtype_code(x), ldx, n)
-        tail = (_ptr(bias), ACTS[act], _ptr(residual), ldr, y.data_ptr(), _dtype_code(y), ldy,
-                ws.data_ptr(), ws.numel() * ws.element_size(), _stream(dev))
+                bits, group, d_out, d_in, _addr(mul_in), _addr(mul_out), _addr(q28_in),
+                _addr(q28_out), flags, x.data_ptr(), _dtype_code(x), ldx, n)
+        tail = (_addr(bias), ACTS[act], _addr(residual), ldr, y.data_ptr(), _dtype_code(y), ldy,
+                ws.data_ptr(), ws.numel() * ws.element_size(), _handle(dev))
         if offsets is None:
             rc = lib.kronq_online_linear(*head, *tail)
         else:
@@ -546,25 +567,26 @@ def kronq_online_grouped(packed: torch.Tensor, scales: torch.Tensor, zeros: torc
 
 def _cache_sizes(codes: torch.Tensor, params: torch.Tensor):
     """(pages, kv heads, page, dim) of a cache."""
-    if params.dim() != 4 or codes.dim() != 4 or codes.shape[:3] != params.shape[:3] or \
-            params.shape[2] != 2:
+    held, grid = codes.shape, params.shape
+    if len(grid) != 4 or len(held) != 4 or held[:3] != grid[:3] or grid[2] != 2:
         raise ValueError("the cache is codes [pages, kv heads, 2, page * dim / 8] and "
                          "params [pages, kv heads, 2, page]")
     for t in (codes, params):
         if t.dtype not in (torch.int32, torch.uint32) or not t.is_contiguous():
             raise ValueError("codes and params must be contiguous 32-bit words")
-    page = params.shape[3]
-    if page < 1 or codes.shape[3] * 8 % page:
+    pages, kv, _, page = grid
+    if page < 1 or held[3] * 8 % page:
         raise ValueError("codes and params differ in their page")
-    return params.shape[0], params.shape[1], page, codes.shape[3] * 8 // page
+    return pages, kv, page, held[3] * 8 // page
 
 
 def _token_stride(t: torch.Tensor, heads: int, dim: int, name: str) -> int:
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
         raise ValueError(f"{name} must be [tokens, {heads}, {dim}]")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+    if stride[2] != 1 or (heads > 1 and stride[1] != dim):
         raise ValueError(f"the heads of a token of {name} must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else heads * dim
+    return stride[0] if shape[0] > 1 else heads * dim
 
 
 def kronq_cache_empty(pages: int, kv_heads: int, dim: int, page: int = 64, device="cuda"):
@@ -588,11 +610,11 @@ def kronq_cache_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, co
     _typed(slots, torch.int64, (n,), "slots")
     _typed(k_hat, torch.float32, (n, kv, dim), "k_hat")
     _typed(v_hat, torch.float32, (n, kv, dim), "v_hat")
-    with torch.cuda.device(dev):
+    with _guard(dev):
         rc = load().kronq_cache_append(k.data_ptr(), v.data_ptr(), _dtype_code(k), ldk, ldv, n, kv,
                                        dim, slots.data_ptr(), codes.data_ptr(), params.data_ptr(),
-                                       pages, page, int(rotate), _ptr(k_hat), _ptr(v_hat),
-                                       _stream(dev))
+                                       pages, page, int(rotate), _addr(k_hat), _addr(v_hat),
+                                       _handle(dev))
     _check(rc, "kronq_cache_append")
 
 
@@ -631,15 +653,15 @@ def kronq_cache_attention(q: torch.Tensor, codes: torch.Tensor, params: torch.Te
         return out
     most = max_new if max_new is not None else 1 if starts is None else n
     ldt = table.stride(0) if seqs > 1 else table.shape[1]
-    with torch.cuda.device(dev):
+    with _guard(dev):
         if ws is None:
             ws = torch.empty(lib.kronq_workspace_bytes(OP_ATTENTION, heads, dim, n),
                              dtype=torch.uint8, device=dev)
         rc = lib.kronq_cache_attention(
             q.data_ptr(), ldq, n, heads, kv, dim, codes.data_ptr(), params.data_ptr(), pages, page,
-            table.data_ptr(), ldt, table.shape[1], lengths.data_ptr(), seqs, _ptr(starts),
+            table.data_ptr(), ldt, table.shape[1], lengths.data_ptr(), seqs, _addr(starts),
             int(most), dim ** -0.5 if scale is None else float(scale), int(rotate), out.data_ptr(),
-            ldo, ws.data_ptr(), ws.numel() * ws.element_size(), _stream(dev))
+            ldo, ws.data_ptr(), ws.numel() * ws.element_size(), _handle(dev))
     _check(rc, "kronq_cache_attention")
     return out
 
