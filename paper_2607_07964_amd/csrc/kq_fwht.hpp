@@ -25,11 +25,6 @@ __device__ __forceinline__ float dpp_mov(float x) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true));
 }
 
-template <int CTRL>
-__device__ __forceinline__ int dpp_movi(int x) {
-  return __builtin_amdgcn_mov_dpp(x, CTRL, 0xf, 0xf, true);
-}
-
 // One stage x <- x + s y (y the partner's value, s the sign of the lane's own half) on eight registers:
 // right for the lower element and the negative for the upper one, so that after several of them a
 // lane's values have the product of its signs, which the callers multiply by once. (As asm: from the builtin the compiler makes two moves and the

@@ -92,25 +92,30 @@ __device__ __forceinline__ RowGrid row_grid(const float (&x)[8], int chunk, int 
   // up to bf16: 45 of the 52 bits of the fraction go
   const uint64_t up = (__builtin_bit_cast(uint64_t, wide) + ((uint64_t(1) << 45) - 1)) &
                       ~((uint64_t(1) << 45) - 1);
-  const double scale = __builtin_bit_cast(double, up);
+  const double scale = __builtin_bit_cast(double, up), inv = 1.0 / scale;
   const double zero = fmin(rint(-lo / scale), 15.0);
   RowGrid g{0, float(scale), float(zero), bad != 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const double c = bad ? 0.0 : fmin(fmax(rint(r[i] / scale) + zero, 0.0), 15.0);
+    const double t = r[i] * inv;  // good to 2^-51: rint(t) is rint(r / scale) unless t is next to a
+    double n = rint(t);           // half, where the quotient itself decides
+    if (fabs(fabs(t - n) - 0.5) < 1e-12) n = rint(r[i] / scale);
+    const double c = bad ? 0.0 : fmin(fmax(n + zero, 0.0), 15.0);
     g.word |= uint32_t(int(c)) << (4 * i);
   }
   return g;
 }
 
 // dim / 8 lanes take a row, eight values each. The grid is worked out in fp32 and kept where fp32
-// must agree with fp64, which settles the rest (some 3 rows of 100; all of it in fp64 was bound by
-// its arithmetic). With range = hi - lo >= max |f| and f = D^(1/2) r the transform before its norm, its
-// log2(D) stages round by at most 2^-24 |x|_1 each, and |x|_1 <= D^(1/2) |x|_2 <= D^(1/2) max |f|, so
-//   |error of f| <= 7 2^-24 11.4 range < 4.8e-6 range: of range itself < 1.1e-5 with the products
-//     after it, less than 192 steps of a 24-bit fraction (a scale ends at 16 of them: 256 are kept clear),
-//   |error of r / scale| < 15 4.8e-6 + 15 2^-22 < 8e-5: halves are kept clear by 1e-4.
-// 64000 tokens TOKENS_FIGURE
+// must agree with fp64, which settles the rest (some rows of 100). The transform before its norm, f,
+// has log2(D) <= 7 stages; each rounds by at most 2^-24 of its result in the 2-norm and all later ones
+// scale that as they scale the result, so |error of f|_2 <= 7 2^-24 |f|_2. With t = r / scale, whose
+// range is 14.8 to 15,
+//   |error of t| < 4.2e-7 |t|_2 + 3 2^-24 15: halves are kept clear by 4.24e-7 |t|_2 + 4e-6;
+//   the range's error is twice that of a value, |t|_2 steps of a 24-bit fraction and some for the
+//     products after it: where the scale is cut, 16 of those bits, |t|_2 + 8 steps are kept clear.
+// 16000 tokens of 8 heads of 128 (213 MB with what the cache holds): 53 us, 4.0 TB/s; all of it in fp64
+// was bound by that arithmetic, 72 us.
 template <typename T, int DIM>
 __global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
   constexpr int LPR = DIM / 8, RPW = 256 / LPR;  // lanes per row, rows per workgroup
@@ -120,12 +125,12 @@ __global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
   const int64_t rows = A.n_tokens * A.n_kv * 2;
   if (row >= rows) return;  // (whole groups of LPR lanes)
   const int part = int(row & 1);
-  const int64_t th = row >> 1, token = th / A.n_kv;
-  const int head = int(th % A.n_kv);
+  const uint32_t th = uint32_t(row >> 1), token = th / uint32_t(A.n_kv);  // (at most 2^31 of them)
+  const int head = int(th - token * uint32_t(A.n_kv));
   const int64_t slot = A.slots[token];
   if (slot < 0 || slot >= A.n_slots) return;
-  const T* src = static_cast<const T*>(part ? A.v : A.k) + token * (part ? A.ldv : A.ldk) +
-                 int64_t(head) * DIM + chunk * 8;
+  const T* src = static_cast<const T*>(part ? A.v : A.k) +
+                 int64_t(token) * (part ? A.ldv : A.ldk) + int64_t(head) * DIM + chunk * 8;
   float x[8], f[8];
   if constexpr (sizeof(T) == 2) {
     const uint4 w = *reinterpret_cast<const uint4*>(src);
@@ -153,41 +158,43 @@ __global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
     if constexpr (LPR == 16) stage_lane8(f, (chunk & 8) ? -1.f : 1.f);
     norm = float(A.norm), sign = (__popc(unsigned(chunk)) & 1) ? -1.f : 1.f;
   }
-  float lo = f[0], hi = f[0], nan = 0.f;
+  float lo = f[0], hi = f[0];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, f[i]), hi = fmaxf(hi, f[i]);
-    nan = fmaf(f[i], 0.f, nan);  // NaN if any of them is NaN or infinite
-  }
+  for (int i = 1; i < 8; ++i) lo = fminf(lo, f[i]), hi = fmaxf(hi, f[i]);
   const float least = sign < 0.f ? -hi : lo, most = sign < 0.f ? -lo : hi;
   lo = fminf(least, 0.f), hi = fmaxf(most, 0.f);
   auto join = [&](auto other) {
-    lo = fminf(lo, other(lo)), hi = fmaxf(hi, other(hi)), nan += other(nan);
+    lo = fminf(lo, other(lo)), hi = fmaxf(hi, other(hi));
   };
   join([](float v) { return dpp_mov<0xB1>(v); });
   join([](float v) { return dpp_mov<0x4E>(v); });
   join([](float v) { return dpp_mov<0x141>(v); });
   if constexpr (LPR == 16) join([](float v) { return dpp_mov<0x128>(v); });
-  const float range = hi - lo, wide = fmaxf(range * (norm / 15.f), 0x1p-100f);
-  const uint32_t bits = __float_as_uint(wide);
+  const float range = hi - lo, step = range * (norm / 15.f);
+  const uint32_t bits = __float_as_uint(fmaxf(step, 0x1p-100f));
   RowGrid g;
   g.scale = __uint_as_float((bits + 0xFFFFu) & 0xFFFF0000u);
   const float inv = norm / g.scale, to = inv * sign, z = -lo * inv;
   g.zero = fminf(rintf(z), 15.f), g.bad = false, g.word = 0;
-  float far = fabsf(z - rintf(z));  // from the next whole number
+  float far = fabsf(z - rintf(z)), sum = 0.f;  // from the next whole number; |t|_2 squared
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float t = f[i] * to, n = rintf(t);
-    far = fmaxf(far, fabsf(t - n));
+    far = fmaxf(far, fabsf(t - n)), sum = fmaf(t, t, sum);
     const float c = fminf(fmaxf(n + g.zero, 0.f), 15.f);
     g.word |= uint32_t(int(c)) << (4 * i);
   }
-  const uint32_t low = bits & 0xFFFFu;
-  int sure = far < 0.4999f && low - 256u < 65536u - 512u && range <= 3.0e38f && nan == 0.f;
-  sure &= dpp_movi<0xB1>(sure);
-  sure &= dpp_movi<0x4E>(sure);
-  sure &= dpp_movi<0x141>(sure);
-  if constexpr (LPR == 16) sure &= dpp_movi<0x128>(sure);
+  auto row_of = [&](auto other) { far = fmaxf(far, other(far)), sum += other(sum); };
+  row_of([](float v) { return dpp_mov<0xB1>(v); });
+  row_of([](float v) { return dpp_mov<0x4E>(v); });
+  row_of([](float v) { return dpp_mov<0x141>(v); });
+  if constexpr (LPR == 16) row_of([](float v) { return dpp_mov<0x128>(v); });
+  // (a value that is not finite makes the range infinite or the sum NaN; step below the least scale
+  // is not cut)
+  const float low = float(bits & 0xFFFFu), clear = fminf(low, 65536.f - low) - 8.f;
+  const float half = 0.5f - 4e-6f - far;
+  const bool sure = half > 0.f && half * half > 1.8e-13f * sum && range <= 3.0e38f &&
+                    (step < 0x1.fp-101f || (clear > 0.f && clear * clear > sum));
   if (!sure) g = row_grid<LPR>(x, chunk, A.rotate, A.norm);
   // a row with a value that is not finite reads as NaN
   if (g.bad) g.scale = __uint_as_float(0x7FC00000u);
@@ -200,7 +207,7 @@ __global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
         __float_as_uint(g.scale) | (g.bad ? 0u : uint32_t(int(g.zero)));
   float* out = part ? A.v_hat : A.k_hat;
   if (out) {
-    out += th * DIM + chunk * 8;
+    out += int64_t(th) * DIM + chunk * 8;
     float hat[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) hat[i] = g.scale * (float((g.word >> (4 * i)) & 15u) - g.zero);
