@@ -211,14 +211,20 @@ __device__ __forceinline__ void across_columns(float (&x)[C], float (&y)[C], Put
 }
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-// A lane's share of the factor (or its transpose) as the A operand of mix28
+// The factor in LDS (its rows 28 floats apart; as loads of every lane's own values it was a third of
+// the time of linear_in), and a lane's share of it, or of its transpose, as the A operand of mix28
+template <int THR>
+__device__ __forceinline__ void stage28(float* lds, const float* __restrict__ q28, int tid) {
+  for (int i = tid; i < 784; i += THR) lds[i] = q28[i];
+}
 template <bool TRANS>
-__device__ __forceinline__ void load28(float (&q)[14], const float* __restrict__ q28, int lane) {
+__device__ __forceinline__ void load28(float (&q)[14], const float* lds, int lane) {
 #pragma unroll
   for (int s = 0; s < 14; ++s) {
     const int k = 2 * s + (lane >> 5), n = lane & 31, a = n < 28 ? n : 27;
-    q[s] = q28[TRANS ? k * 28 + a : a * 28 + k];  // (rows 28 to 31 are not used)
+    q[s] = lds[TRANS ? k * 28 + a : a * 28 + k];  // (rows 28 to 31 are not used)
   }
 }
 
@@ -286,7 +292,7 @@ __global__ __launch_bounds__(threads(C)) void linear_in(LinearIn A, int table_bl
   extern __shared__ __attribute__((aligned(16))) float buf[];  // the row, when rotated
   constexpr int THR = threads(C), WAVES = THR / 64;
   __shared__ float red[WAVES];
-  __shared__ int sh[THR];
+  __shared__ int sh[THR];  // (at least 784 for the factor)
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (int(blockIdx.x) < lead) {
     if (int(blockIdx.x) < table_blocks) fill_table(A, blockIdx.x);
@@ -310,8 +316,8 @@ __global__ __launch_bounds__(threads(C)) void linear_in(LinearIn A, int table_bl
   if constexpr (C > 0) {
     const int cols = A.turn.cols;
     if constexpr (C % 28 == 0) {
-      float q[14];
-      load28<false>(q, A.q28 + int64_t(expert) * 784, lane);
+      float* const factor = reinterpret_cast<float*>(sh);
+      stage28<THR>(factor, A.q28 + int64_t(expert) * 784, tid);
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         const int j = 8 * (tid + THR * n);
@@ -328,6 +334,8 @@ __global__ __launch_bounds__(threads(C)) void linear_in(LinearIn A, int table_bl
         *reinterpret_cast<float4*>(buf + j + 4) = make_float4(o[4], o[5], o[6], o[7]);
       }
       __syncthreads();
+      float q[14];
+      load28<false>(q, factor, lane);
       // (in place: a wave reads all of its 32 places before it writes them)
       mix28<C / 28>(buf, A.turn.m, q, wave, WAVES, lane, [&](int i, float v) { buf[i] = v; });
     } else {
@@ -562,20 +570,23 @@ struct Products {
 };
 
 // The epilogue on the row in LDS, times unit and the sign that its octets are left with: the elements
-// of places p and p + 1 of every column c from c0 on, c1 apart. A loop, and not unrolled: the
+// of places p and p + 1 of every column c from c0 on, c1 apart, of the count elements from first on
+// that buf holds. A loop, and not unrolled: the
 // activations' code is long, a row is over before it comes from memory once (46 us for rows of 14336
 // with 56 copies of it, for 23 rows and more alike).
 template <typename T>
 __device__ __forceinline__ void finish_row(const LinearOut& A, const float* buf, int64_t row,
-                                           int expert, float unit, int p, int c0, int c1) {
+                                           int expert, float unit, int p, int c0, int c1, int first,
+                                           int count) {
   const int d = int(A.d_out), cols = A.turn.cols;
-  const float* const mul = A.mul ? A.mul + int64_t(expert) * d : nullptr;
-  const float* const bias = A.bias ? A.bias + int64_t(expert) * d : nullptr;
-  const T* const res = A.residual ? static_cast<const T*>(A.residual) + row * A.ldr : nullptr;
-  T* const y = static_cast<T*>(A.y) + row * A.ldy;
+  const float* const mul = A.mul ? A.mul + int64_t(expert) * d + first : nullptr;
+  const float* const bias = A.bias ? A.bias + int64_t(expert) * d + first : nullptr;
+  const T* const res =
+      A.residual ? static_cast<const T*>(A.residual) + row * A.ldr + first : nullptr;
+  T* const y = static_cast<T*>(A.y) + row * A.ldy + first;
   const float up = unit * octet_sign(p >> 3, cols);
 #pragma unroll 1
-  for (unsigned j = c0 * cols + p; int(j) < d; j += c1 * cols) {
+  for (unsigned j = c0 * cols + p; int(j) < count; j += c1 * cols) {
     const float2 v = *reinterpret_cast<const float2*>(buf + j);
     float a = v.x * up, b = v.y * up, f, g;
     if (mul) load2(mul + j, f, g), a *= f, b *= g;
@@ -610,8 +621,8 @@ __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
     expert = expert_of(A.offsets, A.n_experts, row);
     if (expert < 0) return;
   }
-  float q[14];
-  if constexpr (C % 28 == 0) load28<true>(q, A.q28 + int64_t(expert) * 784, lane);
+  __shared__ float factor[C % 28 == 0 ? 784 : 1];
+  if constexpr (C % 28 == 0) stage28<THR>(factor, A.q28 + int64_t(expert) * 784, tid);
   const Products<TP> products(A, row, expert);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
@@ -631,10 +642,13 @@ __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
   __syncthreads();
   const float unit = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
   if constexpr (C % 28 == 0) {
+    float q[14];
+    load28<true>(q, factor, lane);
     mix28<C / 28>(buf, A.turn.m, q, wave, WAVES, lane, [&](int i, float v) { buf[i] = v; });
     __syncthreads();
     const int half = cols / 2;  // (a power of two from 4 on)
-    finish_row<T>(A, buf, row, expert, unit, 2 * (tid & (half - 1)), tid / half, THR / half);
+    finish_row<T>(A, buf, row, expert, unit, 2 * (tid & (half - 1)), tid / half, THR / half, 0,
+                  d);
   } else {
     const int p = 2 * tid;
     if (p >= cols) return;
@@ -647,8 +661,90 @@ __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
     across_columns<C>(u, w, [&](int c, float a, float b) {
       *reinterpret_cast<float2*>(buf + c * cols + p) = make_float2(a, b);
     });
-    finish_row<T>(A, buf, row, expert, unit, p, 0, 1);  // (of what this thread has put there)
+    finish_row<T>(A, buf, row, expert, unit, p, 0, 1, 0, d);  // (of what this thread has put there)
   }
+}
+
+// A few rows of 28 m: four workgroups to a row, 7 segments each, where one to a row would leave most
+// CUs idle (a row of 14336 is 16 us of work for one). Each sums all products of the row, so the factor
+// comes first here: 16 x 16 tiles of it on the matrix cores take a workgroup's 7 rows of the factor
+// (PARTS_FIGURE).
+constexpr int PARTS = 4;
+template <typename TP, typename T, int B>
+__global__ __launch_bounds__(1024) void linear_out_part(LinearOut A) {
+  extern __shared__ __attribute__((aligned(16))) float buf[];  // the row, then the 7 segments
+  __shared__ float factor[784];
+  constexpr int WAVES = 16;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int d = int(A.d_out), cols = A.turn.cols, m = A.turn.m;
+  const int64_t row = blockIdx.x / PARTS;
+  const int first = 7 * int(blockIdx.x % PARTS);  // segment
+  int expert = 0;
+  if (A.offsets) {
+    expert = expert_of(A.offsets, A.n_experts, row);
+    if (expert < 0) return;
+  }
+  stage28<1024>(factor, A.q28 + int64_t(expert) * 784, tid);
+  const Products<TP> products(A, row, expert);
+#pragma unroll 1
+  for (int j = 8 * tid; j < d; j += 8192) {
+    float v[8];
+    products.sum8(j, v);
+    *reinterpret_cast<float4*>(buf + j) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(buf + j + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  __syncthreads();
+  {
+    const int n = lane & 15, quad = lane >> 4;
+    float q[7];
+#pragma unroll
+    for (int s = 0; s < 7; ++s) q[s] = factor[(4 * s + quad) * 28 + first + (n < 7 ? n : 6)];
+    // (in place: a wave reads all of its 16 places before it writes them)
+    for (int p0 = 16 * wave; p0 < cols; p0 += 16 * WAVES) {
+      const int p = p0 + n, pc = p < cols ? p : cols - 1;
+      f32x4_t o[B] = {};
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int s = 0; s < 7; ++s)
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(q[s], buf[(4 * s + quad) * m + 512 * b + pc],
+                                                      o[b], 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int a = 4 * quad + r;
+        if (a >= 7 || p >= cols) continue;
+        if constexpr (B == 2) {
+          buf[a * m + p] = o[0][r] + o[1][r];
+          buf[a * m + p + 512] = o[0][r] - o[1][r];
+        } else {
+          buf[a * m + p] = o[0][r];
+        }
+      }
+    }
+  }
+  __syncthreads();
+  for (int at = 512 * wave; at < 7 * m; at += 512 * WAVES) {  // (uniform over the wave)
+    const int j = at + 8 * octet_of(lane);
+    float v[8] = {};
+    if (j < 7 * m) load8(buf + j, v);
+    const bool full = cols == 512;
+    if (full)
+      inside_column<1, true>(v, lane, cols);
+    else
+      inside_column<1, false>(v, lane, cols);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int q = at + (full ? quad_at<false, true>(lane, h) : quad_at<false, false>(lane, h));
+      if (q < 7 * m)
+        *reinterpret_cast<float4*>(buf + q) =
+            make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+    }
+  }
+  __syncthreads();
+  const float unit = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
+  const int half = cols / 2;  // (a power of two from 4 on)
+  finish_row<T>(A, buf, row, expert, unit, 2 * (tid & (half - 1)), tid / half, 1024 / half,
+                first * m, 7 * m);
 }
 
 // Rows without a transform, and transforms whose columns are shorter than an octet (cols: 1, 2 or 4
@@ -739,6 +835,14 @@ int out_typed(LinearOut a, hipStream_t s) {
     return launch("linear_out", linear_out_any<TP, T>, grid, dim3(256), 0, s, a);
 #define KQ_OUT(C_, F_) \
   launch("linear_out", linear_out<TP, T, C_, F_>, grid, dim3(threads(C_)), size_t(a.d_out) * 4, s, a)
+  if (a.turn.has28 && a.n_rows * PARTS <= device_cus()) {
+    const dim3 parts(static_cast<unsigned>(a.n_rows * PARTS));
+    return a.turn.m == 1024
+               ? launch("linear_out", linear_out_part<TP, T, 2>, parts, dim3(1024),
+                        size_t(a.d_out) * 4, s, a)
+               : launch("linear_out", linear_out_part<TP, T, 1>, parts, dim3(1024),
+                        size_t(a.d_out) * 4, s, a);
+  }
   const bool full = a.turn.cols == 512;
   switch (a.d_out / a.turn.cols) {
     case 1:
