@@ -113,6 +113,8 @@ int linear_common(const kq::LinearJob& j, void* ws, size_t ws_bytes, void* strea
   KQ_REQUIRE(j.scales && j.zeros && aligned(j.scales, 4) && aligned(j.zeros, 4) &&
                  j.ldsz >= j.d_in / j.group,
              KRONQ_ERR_INVALID_ARG, "bad scales or zeros");
+  KQ_REQUIRE(j.ldp <= (1 << 20) && j.ldsz <= (1 << 20), KRONQ_ERR_UNSUPPORTED,
+             "ldp and ldsz must be at most 2^20");
   KQ_REQUIRE(aligned(j.mul_in, 16) && aligned(j.mul_out, 16) && aligned(j.bias, 4),
              KRONQ_ERR_INVALID_ARG, "mul_in and mul_out must be 16-byte aligned, bias 4");
   KQ_REQUIRE(valid_dtype(j.x_dtype) && valid_dtype(j.y_dtype), KRONQ_ERR_INVALID_ARG,

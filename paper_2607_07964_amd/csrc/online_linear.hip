@@ -30,6 +30,10 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+#define KQ_RSRC(base, bytes) \
+  __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(static_cast<const void*>(base)), 0, int(bytes), \
+                                    0x00027000)
 #define KQ_LDS(p) ((__attribute__((address_space(3))) void*)(p))
 
 using Tile = LinearTile;
@@ -41,6 +45,8 @@ __host__ __device__ inline int64_t most_tiles(int64_t n_rows, int64_t n_experts,
   const int64_t e = n_experts < n_rows ? n_experts : n_rows;
   return (cdiv(n_rows, 32) + e - 1) / nt + e;
 }
+
+constexpr int BLOCK = 256;  // rows of W of an item
 
 // ---- 2. products ---------------------------------------------------------------------------------
 struct MmArgs {
@@ -163,6 +169,232 @@ __device__ __forceinline__ void load_codes(uint32_t* w, const uint32_t* p) {
   }
 }
 
+// Few rows: the codes' way from memory bounds it. A workgroup of eight waves, one per CU, takes 256
+// rows of W (32 a wave) and a tile of NT units; everything comes straight to LDS in whole lines, and
+// the lanes take their own rows' codes from there. (Codes that each lane loads from its own row are
+// one L1 access a lane: those bound it, 66 us for 8 experts of 14336 x 4096 at 4 bits with 32 rows
+// that take FEW_US now.) In LDS:
+//   x': RG groups of NP pieces (unit, plane) of 8 KB in fragment order, one step of 16 columns a wave;
+//   codes: CB batches of BG groups, of LB bytes a row: with rows of 128 bytes piece p of 16 stands at
+//     p ^ (row & 7), so that eight lanes reading theirs meet in no bank;
+//   scales and zeros: two sets of four groups, [row][group].
+// One barrier a group, in its middle: it publishes the next group's operands and frees those of the
+// group before, which the loads after it then fill. vmcnt counts in order, and the loads below leave in
+// an order that is the same for every group of a batch, so `newer` tells at compile time how many may
+// still be out; loads past the end of the range leave too (out of bounds: they read nothing).
+constexpr int newer(int u, int np, int rg, int cb, int bg, int cl) {  // group u of a batch
+  int x = 0, c = 0;  // loads that left after those of the next group's x', and of its codes
+  for (int back = rg - 2; back >= 1; --back)  // (the middle of the group `back` groups ago)
+    x += (back < rg - 2 ? np : 0) + ((u - back) % bg == 0 ? cl : 0);  // (codes after x')
+  for (int back = (cb - 1) * bg - 2; back >= 1; --back) c += np + ((u - back) % bg == 0 ? cl : 0);
+  return u == bg - 1 && c < x ? c : x;
+}
+
+template <int BITS, int NT, int PLANES>
+__global__ __launch_bounds__(512, 2) void linear_few(MmArgs A) {
+  constexpr int NP = NT * PLANES, XG = NP * 2048;  // (dwords of a group of x')
+  constexpr int RG = NP == 1 ? 4 : 3, CB = 3;
+  constexpr int LB = BITS == 3 ? 96 : 128, PPR = LB / 16, BG = LB / (16 * BITS);
+  constexpr int CL = BLOCK * PPR / 512;  // loads of a batch of codes per wave
+  constexpr int CODES = RG * XG, PARAMS = CODES + CB * BLOCK * LB / 4, SET = BLOCK * 4 * 2;
+  __shared__ __attribute__((aligned(16))) uint32_t lds[PARAMS + 2 * SET];
+  static_assert(sizeof(lds) <= 163840, "160 KB a CU");
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // (workers that share an XCD stand next to one another in the deal, as below)
+  const int W = int(gridDim.x), id = int(blockIdx.x & 7) * (W >> 3) + int(blockIdx.x >> 3);
+  const int ntiles = A.tiles ? A.tiles[0].expert : int(cdiv(A.n_rows, 32 * NT));
+  const int items = ntiles * A.row_blocks;
+  const LinearDeal deal = linear_deal(items, A.ng, W);
+  const int rest = items - deal.full * W;
+  int round = 0, ua = id * deal.per;  // next group of the rest
+  const int ub = ua + deal.per < rest * A.ng ? ua + deal.per : rest * A.ng;
+  for (;;) {
+    int item, g0 = 0, g1 = A.ng;
+    if (round < deal.full) {
+      item = round++ * W + id;
+    } else if (ua < ub) {
+      const int r = ua / A.ng;
+      item = deal.full * W + r;
+      g0 = ua - r * A.ng;
+      g1 = g0 + (ub - ua) < A.ng ? g0 + (ub - ua) : A.ng;
+      ua += g1 - g0;
+    } else {
+      break;
+    }
+    const int rb = item % A.row_blocks, ti = item / A.row_blocks;
+    const Tile t = A.tiles ? A.tiles[1 + ti] : Tile{0, ti * NT, 0, int(A.n_rows)};
+    const int last = (t.hi - 1) >> 5;  // last unit
+    const int ngr = g1 - g0;
+    const int64_t row0 = int64_t(t.expert) * A.d_out + int64_t(rb) * BLOCK;  // of W
+    const int left = int(A.d_out - int64_t(rb) * BLOCK);
+    const int n_last = (left < BLOCK ? left : BLOCK) - 1;  // last row of W here
+    // x'
+    auto issue_x = [&](int g) {  // past the end: the last group again, never read
+      const int at = ((g0 + (g < ngr ? g : ngr - 1)) * 8 + wave) * 1024;
+      uint32_t* const dst = lds + (g % RG) * XG + wave * 256;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int un = t.unit + p / PLANES;
+        const uint16_t* const rows =
+            A.xf + (p % PLANES) * A.plane + (un < last ? un : last) * int64_t(A.ng) * 4096;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(KQ_RSRC(rows, A.ng * 8192), KQ_LDS(dst + p * 2048), 16,
+                                                 lane * 16, at, 0, 0);
+      }
+    };
+    // codes
+    const auto code_src = KQ_RSRC(A.packed + row0 * A.ldp,
+                               (int64_t(n_last) * A.ldp + A.ng * 4 * BITS) * 4);
+    int code_at[CL];
+#pragma unroll
+    for (int i = 0; i < CL; ++i) {
+      const int idx = i * 512 + tid, n = idx / PPR, slot = idx % PPR;
+      const int piece = PPR == 8 ? slot ^ (n & 7) : slot;
+      code_at[i] = (n < n_last ? n : n_last) * int(A.ldp * 4) + g0 * 16 * BITS + piece * 16;
+    }
+    auto issue_codes = [&](int b) {
+      uint32_t* const dst = lds + CODES + ((b + CB) % CB) * (BLOCK * LB / 4) + wave * 256;
+      const bool in = b >= 0 && b * BG < ngr;
+#pragma unroll
+      for (int i = 0; i < CL; ++i) {
+        const int at = in ? code_at[i] + b * LB : -256;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(code_src, KQ_LDS(dst + i * 2048), 16, at, 0, 0, 0);
+      }
+    };
+    // scales and zeros of groups g to g + 3
+    const int szn = (n_last * int(A.ldsz) + A.ng / A.gpq) * 4;
+    const auto s_src = KQ_RSRC(A.scales + row0 * A.ldsz, szn), z_src = KQ_RSRC(A.zeros + row0 * A.ldsz, szn);
+    auto issue_params = [&](int g) {
+      uint32_t* const dst = lds + PARAMS + ((g >> 2) & 1) * SET + wave * 64;
+      const int k = g + (tid & 3);
+      const unsigned q = unsigned(g0 + (k < ngr ? k : ngr - 1)) / unsigned(A.gpq);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int n = i * 128 + (tid >> 2);
+        const int at = (n < n_last ? n : n_last) * int(A.ldsz * 4) + int(q) * 4;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(s_src, KQ_LDS(dst + i * 512), 4, at, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(z_src, KQ_LDS(dst + 1024 + i * 512), 4, at, 0, 0, 0);
+      }
+    };
+    // what a lane takes of a group: its row's codes of half of the columns (two chunks of 32), scale and
+    // fp16 pair of -(1024 + zero)
+    const int mine = 32 * wave + (lane & 31), h = lane >> 5;
+    auto read_codes = [&](uint32_t (&w)[2 * BITS], int g, auto kc) {  // kc: group of its batch
+      constexpr int k = decltype(kc)::value;
+      const uint32_t* const c = lds + CODES + (g / BG % CB) * (BLOCK * LB / 4) + mine * (LB / 4);
+      if constexpr (BITS == 3) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          const u32x2_t v = *reinterpret_cast<const u32x2_t*>(c + k * 12 + h * 6 + 2 * i);
+          w[2 * i] = v[0], w[2 * i + 1] = v[1];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < BITS / 2; ++i) {
+          const int piece = k * BITS + h * (BITS / 2) + i;
+          const u32x4_t v = *reinterpret_cast<const u32x4_t*>(c + 4 * (piece ^ (mine & 7)));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+        }
+      }
+    };
+    auto read_params = [&](float& s, uint32_t& nz, int g) {
+      const uint32_t* const c = lds + PARAMS + ((g >> 2) & 1) * SET + mine * 4 + (g & 3);
+      s = __uint_as_float(c[0]);
+      const _Float16 z = _Float16(-1024.f - __uint_as_float(c[1024]));
+      nz = u2(f16x2_t{z, z});
+    };
+    u32x4_t a[2][NP];
+    auto frags = [&](int g, int q) {
+      const uint32_t* const buf = lds + (g % RG) * XG + lane * 4 + q * 256;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) a[q & 1][i] = *reinterpret_cast<const u32x4_t*>(buf + i * 2048);
+    };
+    f32x16_t acc[NT] = {}, sum[NT] = {};
+    uint32_t cw[2 * BITS], cw1[2 * BITS], sz, sz1;
+    float sc, sc1;
+    auto group = [&](int g, auto uc) {
+      constexpr int u = decltype(uc)::value;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        if (q == 4) {
+          wait_vm<newer(u, NP, RG, CB, BG, CL)>();
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          issue_x(g + RG - 1);
+          if constexpr (u == 0) issue_codes(g / BG + CB - 1);
+          if ((g & 3) == 0) issue_params(g + 4);
+          __builtin_amdgcn_sched_barrier(0);
+          read_codes(cw1, g + 1, std::integral_constant<int, (u + 1) % BG>{});
+          read_params(sc1, sz1, g + 1);
+        }
+        frags(q < 7 ? g : g + 1, (q + 1) & 7);
+        const u32x4_t b = spread_int<BITS>(cw + (q >> 2) * BITS, q & 3, sz);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          if constexpr (PLANES == 2) sum[i] = mfma(a[q & 1][2 * i + 1], b, sum[i]);
+          sum[i] = mfma(a[q & 1][PLANES * i], b, sum[i]);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (else every step's operands are read at once)
+      }
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) acc[i][k] = fmaf(sc, sum[i][k], acc[i][k]), sum[i][k] = 0.f;
+#pragma unroll
+      for (int k = 0; k < 2 * BITS; ++k) cw[k] = cw1[k];
+      sc = sc1, sz = sz1;
+    };
+    issue_params(0);
+    __builtin_amdgcn_sched_barrier(0);
+    // (the loads of the middles before the first group)
+    constexpr int FIRST = RG - 1 > (CB - 1) * BG ? RG - 1 : (CB - 1) * BG;
+#pragma unroll
+    for (int s = -FIRST; s < 0; ++s) {
+      if (s + RG - 1 >= 0) issue_x(s + RG - 1);
+      if (s % BG == 0) issue_codes(s / BG + CB - 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    wait_vm<newer(BG - 1, NP, RG, CB, BG, CL)>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read_codes(cw, 0, std::integral_constant<int, 0>{});
+    read_params(sc, sz, 0);
+    frags(0, 0);
+    for (int g = 0; g < ngr; g += BG) {
+      group(g, std::integral_constant<int, 0>{});
+      if constexpr (BG > 1) {
+        if (g + 1 < ngr) group(g + 1, std::integral_constant<int, 1>{});
+      }
+      if constexpr (BG > 2) {
+        if (g + 2 < ngr) group(g + 2, std::integral_constant<int, 2>{});
+        if (g + 3 < ngr) group(g + 3, std::integral_constant<int, 3>{});
+      }
+    }
+    wait_vm<0>();  // (loads past the end still write to LDS)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    // a worker that began inside an item keeps its part
+    const int64_t ld = g0 > 0 ? BLOCK : A.ld, n = int64_t(rb) * BLOCK + mine;
+    float* const part =
+        g0 > 0 ? static_cast<float*>(A.kept) + (int64_t(id) * NT - t.unit) * 32 * BLOCK - rb * BLOCK
+               : static_cast<float*>(A.part);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int mu = (t.unit + i) * 32, m0 = mu + 4 * h;
+      float* p = part + int64_t(m0) * ld + n;
+      const bool whole = mu >= t.lo && mu + 32 <= t.hi;  // (uniform) every row of it is the tile's
+      if (mine > n_last) continue;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const int m = m0 + 8 * (k >> 2) + (k & 3);
+        if (whole || (m >= t.lo && m < t.hi)) *p = acc[i][k];
+        p += (k & 3) == 3 ? 5 * ld : ld;
+      }
+    }
+  }
+}
+
 // A workgroup of four waves takes 128 RT rows of W (32 RT a wave) and a tile of NT units of rows of
 // x'; a lane holds the codes of RT rows of W and half of the columns, 64 of them a stage. x' comes
 // through LDS: a stage is 64 columns (half a group, a chunk of each lane's codes) of NT units in
@@ -181,14 +413,12 @@ __device__ __forceinline__ void load_codes(uint32_t* w, const uint32_t* p) {
 // (not SCALED) come through LDS eight groups at a time for the same reason: 32 rows lie in 32 lines of
 // either. (8 experts of 14336 x
 // 4096 at 4 bits with 32 rows: 76 us that way, 66 now.)
-constexpr int per_cu(int nt, int rt) { return rt == 2 ? 2 : nt == 2 ? 3 : 4; }
-
-template <int BITS, int NT, int PLANES, int RT, bool SCALED>
-__global__ __launch_bounds__(256, per_cu(NT, RT)) void linear_ring(MmArgs A) {
-  constexpr int NP = NT * PLANES, STAGE = NP * 1024, BLOCK = 128 * RT;  // (STAGE: dwords)
-  constexpr int R = NP == 1 ? 8 : 4;  // stages of the ring
-  // groups of a batch of codes: 16 words a lane with RT = 1 (12 with 3 bits), 8 with RT = 2
-  constexpr int BG = RT == 1 ? (BITS == 2 ? 4 : BITS == 8 ? 1 : 2) : BITS == 2 ? 2 : 1;
+template <int BITS, int NT, int PLANES, bool SCALED>
+__global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
+  constexpr int RT = BLOCK / 128;                        // units of 32 rows of W a wave
+  constexpr int NP = NT * PLANES, STAGE = NP * 1024;     // (dwords)
+  constexpr int R = 4;                                   // stages of the ring
+  constexpr int BG = BITS == 2 ? 2 : 1;                  // groups of a batch of codes: 8 words a lane
   constexpr int SG = 8;  // groups of scales and zeros in LDS
   // the ring, then {scale, fp16 pair of -(1024 + zero)} by group and row (one array: with a second one
   // the compiler waits for all loads to LDS before each read)
@@ -227,8 +457,7 @@ __global__ __launch_bounds__(256, per_cu(NT, RT)) void linear_ring(MmArgs A) {
     // uses one that went to a register)
     const uint16_t* const rows = A.xf + (piece % PLANES) * A.plane +
                                  (un < last ? un : last) * int64_t(A.ng) * 4096;
-    const auto src = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(rows), 0, A.ng * 8192,
-                                                       0x00027000);
+    const auto src = KQ_RSRC(rows, A.ng * 8192);
     auto issue = [&](int st) {  // past the end: the last stage again, never read
       const int at = (2 * g0 + (st < nst ? st : nst - 1)) * 4096;
       uint32_t* dst = lds + (st & (R - 1)) * STAGE + piece * 1024;
@@ -385,10 +614,6 @@ __global__ __launch_bounds__(256, per_cu(NT, RT)) void linear_ring(MmArgs A) {
       if constexpr (BG > 1) {
         if (gb + 1 < ngr) pair(std::integral_constant<int, 1>{});
       }
-      if constexpr (BG > 2) {
-        if (gb + 2 < ngr) pair(std::integral_constant<int, 2>{});
-        if (gb + 3 < ngr) pair(std::integral_constant<int, 3>{});
-      }
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -430,8 +655,8 @@ __global__ __launch_bounds__(256, per_cu(NT, RT)) void linear_ring(MmArgs A) {
 constexpr int64_t GEMV_ROWS = 4, GEMV_INPUTS = 32768;
 
 struct Plan {
-  int planes, nt, rt, workers, block;
-  bool scaled;
+  int planes, nt, workers;
+  bool scaled, few;
   float down;
   int64_t tiles, row_blocks;
 };
@@ -444,11 +669,10 @@ Plan make_plan(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts, i
   const int64_t rows = cdiv(n_rows, n_experts);
   p.scaled = p.planes == 1 && rows > 64;
   p.nt = p.scaled ? 4 : rows > 32 ? 2 : 1;
-  p.rt = p.nt * p.planes == 4 ? 2 : 1;
-  p.block = 128 * p.rt;
+  p.few = p.nt * p.planes < 4;
   p.tiles = n_experts == 1 ? cdiv(n_rows, 32 * p.nt) : most_tiles(n_rows, n_experts, p.nt);
-  p.row_blocks = cdiv(d_out, p.block);
-  p.workers = device_cus() / 8 * 8 * per_cu(p.nt, p.rt);
+  p.row_blocks = cdiv(d_out, BLOCK);
+  p.workers = device_cus() / 8 * 8 * (p.few ? 1 : 2);
   // fp16 results: below 2^8 (x') times 2.5 (|c - z| < 1280 of at most 2^-9) times d_in
   p.down = 1.f;
   while (p.scaled && 640.f * float(d_in) * p.down > 65000.f) p.down *= 0.5f;
@@ -473,7 +697,7 @@ Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, i
   w.row_unit = cv.take<float>(size_t(n_rows));
   const size_t size = p.scaled ? 2 : 4;  // of a product
   w.part = cv.take<char>(size_t(n_rows) * size_t(cdiv(d_out, 8) * 8) * size);
-  w.kept = cv.take<char>(size_t(p.workers) * size_t(32 * p.nt) * size_t(p.block) * size);
+  w.kept = cv.take<char>(size_t(p.workers) * size_t(32 * p.nt) * size_t(BLOCK) * size);
   const size_t w_rows = p.scaled ? size_t(n_experts) * size_t(d_out) : 0;
   w.w_unit = cv.take<float>(w_rows);
   w.table = cv.take<uint32_t>(w_rows * size_t(d_in / 128));
@@ -486,12 +710,11 @@ Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, i
 template <int BITS>
 int launch_mm(const MmArgs& a, const Plan& p, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(p.workers));
-#define KQ_MM(NT_, PL_, RT_, SC_) \
-  launch("linear_ring", linear_ring<BITS, NT_, PL_, RT_, SC_>, grid, dim3(256), 0, s, a)
-  if (p.scaled) return KQ_MM(4, 1, 2, true);
-  if (p.planes == 1) return p.nt == 1 ? KQ_MM(1, 1, 1, false) : KQ_MM(2, 1, 1, false);
-  return p.nt == 1 ? KQ_MM(1, 2, 1, false) : KQ_MM(2, 2, 2, false);
-#undef KQ_MM
+  if (p.scaled) return launch("linear_ring", linear_ring<BITS, 4, 1, true>, grid, dim3(256), 0, s, a);
+  if (!p.few) return launch("linear_ring", linear_ring<BITS, 2, 2, false>, grid, dim3(256), 0, s, a);
+#define KQ_FEW(NT_, PL_) launch("linear_few", linear_few<BITS, NT_, PL_>, grid, dim3(512), 0, s, a)
+  return p.planes == 2 ? KQ_FEW(1, 2) : p.nt == 1 ? KQ_FEW(1, 1) : KQ_FEW(2, 1);
+#undef KQ_FEW
 }
 
 }  // namespace
@@ -546,7 +769,7 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
          : j.bits == 3 ? launch_mm<3>(m, p, s)
          : j.bits == 4 ? launch_mm<4>(m, p, s)
                        : launch_mm<8>(m, p, s));
-  o.part = w.part, o.ld = m.ld, o.block = p.block;
+  o.part = w.part, o.ld = m.ld, o.block = BLOCK;
   o.row_unit = w.row_unit, o.unit = 1.f / p.down;
   o.workers = p.workers, o.ng = a.ng, o.nt = p.nt, o.row_blocks = m.row_blocks, o.kept = w.kept;
   o.items = int(p.tiles * p.row_blocks), o.w_unit = p.scaled ? w.w_unit : nullptr;
