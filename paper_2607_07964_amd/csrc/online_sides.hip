@@ -84,27 +84,40 @@ __device__ void list_tiles(const LinearIn& A, int* sh) {
   if (tid == 0) A.tiles[0] = LinearTile{base < A.max_tiles ? base : int(A.max_tiles), 0, 0, 0};
 }
 
-// the table of a workgroup's rows of W: 32 threads take a row
-__device__ void fill_table(const LinearIn& A, int64_t block) {
-  const int64_t row = block * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  const int t = threadIdx.x & 31;
-  if (row >= A.w_rows) return;
+// The table of a workgroup's TABLE_ROWS rows of W, 32 groups at a time, turned in LDS (sh): the rows
+// are read along their groups and the table is written along its rows, in whole lines.
+constexpr int TABLE_ROWS = 32, TABLE_LDS = 32 * (TABLE_ROWS + 1);
+template <int THR>
+__device__ void fill_table(const LinearIn& A, int64_t block, int* sh) {
+  constexpr int PER = THR / TABLE_ROWS;  // threads of a row
+  const int r = threadIdx.x / PER, t = threadIdx.x % PER;
+  const int64_t row0 = block * TABLE_ROWS, row = row0 + r < A.w_rows ? row0 + r : A.w_rows - 1;
   const float *s = A.scales + row * A.ldsz, *z = A.zeros + row * A.ldsz;
   const int nq = A.ng / A.gpq;
   float mx = 0.f;
-  for (int g = t; g < nq; g += 32) mx = fmaxf(mx, fabsf(s[g]));
+  for (int g = t; g < nq; g += PER) mx = fmaxf(mx, fabsf(s[g]));
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  for (int o = 1; o < PER; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
   // s 2^24 / unit in [2^14, 2^15): unit = 2^(e + 10) for a largest scale in [2^e, 2^(e + 1))
   const int e = int(__float_as_uint(mx) >> 23) - 127;
   const int ue = mx > 0.f && e < 128 ? clampi(e + 10, -100, 120) : 0;
   const float up = pow2f(-ue);
-  for (int g = t; g < A.ng; g += 32) {
-    const float sn = s[g / A.gpq] * up;
-    const f16x2_t o = {_Float16(sn * 16777216.f), _Float16(-z[g / A.gpq] * sn)};
-    A.table[int64_t(g) * A.w_rows + row] = __builtin_bit_cast(uint32_t, o);
-  }
   if (t == 0) A.w_unit[row] = pow2f(ue);
+  for (int g0 = 0; g0 < A.ng; g0 += 32) {
+    for (int g = g0 + t; g < g0 + 32 && g < A.ng; g += PER) {
+      const int q = g / A.gpq;
+      const float sn = s[q] * up;
+      const f16x2_t o = {_Float16(sn * 16777216.f), _Float16(-z[q] * sn)};
+      sh[(g - g0) * (TABLE_ROWS + 1) + r] = __builtin_bit_cast(int, o);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * TABLE_ROWS; i += THR) {
+      const int g = i / TABLE_ROWS, to = i % TABLE_ROWS;
+      if (g0 + g < A.ng && row0 + to < A.w_rows)
+        A.table[int64_t(g0 + g) * A.w_rows + row0 + to] = uint32_t(sh[g * (TABLE_ROWS + 1) + to]);
+    }
+    __syncthreads();
+  }
 }
 
 // The octet of a wave's 64 that a lane holds: lanes 4-7 of each 8 in reverse order, so that the
@@ -285,17 +298,20 @@ __device__ __forceinline__ void load8(const float* p, float* v) {
 
 // Threads of a workgroup. A row of 28 m takes most of the LDS of half a CU: 16 waves hide its steps.
 constexpr int threads(int c) { return c && c % 28 == 0 ? 1024 : 256; }
+// (linear_in's short rows need no more, and have twice the workgroups on a CU)
+constexpr int in_threads(int c) { return c == 1 || c == 2 ? 128 : threads(c); }
 
 // C: columns of a rotated row (0: not rotated), of 512 elements with FULL. N: octets a thread ends with.
 template <typename T, int C, int N, bool FULL>
-__global__ __launch_bounds__(threads(C)) void linear_in(LinearIn A, int table_blocks, int lead) {
+__global__ __launch_bounds__(in_threads(C)) void linear_in(LinearIn A, int table_blocks, int lead) {
   extern __shared__ __attribute__((aligned(16))) float buf[];  // the row, when rotated
-  constexpr int THR = threads(C), WAVES = THR / 64;
+  constexpr int THR = in_threads(C), WAVES = THR / 64;
   __shared__ float red[WAVES];
-  __shared__ int sh[THR];  // (at least 784 for the factor)
+  __shared__ int sh[TABLE_LDS];  // (also a workgroup's threads, or the factor)
+  static_assert(TABLE_LDS >= THR && TABLE_LDS >= 784);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (int(blockIdx.x) < lead) {
-    if (int(blockIdx.x) < table_blocks) fill_table(A, blockIdx.x);
+    if (int(blockIdx.x) < table_blocks) fill_table<THR>(A, blockIdx.x, sh);
     if (int(blockIdx.x) == lead - 1 && A.offsets) list_tiles(A, sh);
     return;
   }
@@ -339,8 +355,7 @@ __global__ __launch_bounds__(threads(C)) void linear_in(LinearIn A, int table_bl
       // (in place: a wave reads all of its 32 places before it writes them)
       mix28<C / 28>(buf, A.turn.m, q, wave, WAVES, lane, [&](int i, float v) { buf[i] = v; });
     } else {
-      const unsigned p = 2 * tid;
-      if (int(p) < cols) {
+      for (unsigned p = 2 * tid; int(p) < cols; p += 2 * THR) {
         float u[C], w[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) load2(x + c * cols + p, u[c], w[c]);
@@ -789,11 +804,11 @@ __global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
 template <typename T>
 int in_typed(const LinearIn& a, hipStream_t s) {
   const int cc = a.turn.rotate ? int(a.d_in / a.turn.cols) : 0;
-  const int64_t table_blocks = a.table ? cdiv(a.w_rows, threads(cc) / 32) : 0;
+  const int64_t table_blocks = a.table ? cdiv(a.w_rows, TABLE_ROWS) : 0;
   const int64_t lead = cdiv(table_blocks + (a.offsets ? 1 : 0), 8) * 8;
   const dim3 grid(static_cast<unsigned>(lead + cdiv(a.n_rows, 256) * 256));
 #define KQ_IN(C_, N_, F_)                                                                            \
-  launch("linear_in", linear_in<T, C_, N_, F_>, grid, dim3(threads(C_)), C_ ? size_t(a.d_in) * 4 : 0, s, a, \
+  launch("linear_in", linear_in<T, C_, N_, F_>, grid, dim3(in_threads(C_)), C_ ? size_t(a.d_in) * 4 : 0, s, a, \
          int(table_blocks), int(lead))
   if (!a.turn.rotate) {
     const int64_t n = cdiv(a.d_in, 2048);
