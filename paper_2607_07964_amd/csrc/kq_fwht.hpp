@@ -51,6 +51,29 @@ KQ_DPP_STAGE(stage_mirror8, "row_half_mirror")
 KQ_DPP_STAGE(stage_lane8, "row_ror:8")
 #undef KQ_DPP_STAGE
 
+// The stage of lane xor 16, or 32 (WIDE), on N registers a lane (N even): two of them exchange rows,
+// are added and subtracted, and exchange back.
+template <int N, bool WIDE>
+__device__ __forceinline__ void stage_rows(float (&x)[N]) {
+  auto swap = [](float& a, float& b) {
+    const uint32_t u = __float_as_uint(a), v = __float_as_uint(b);
+    if constexpr (WIDE) {
+      const auto r = __builtin_amdgcn_permlane32_swap(u, v, false, false);
+      a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
+    } else {
+      const auto r = __builtin_amdgcn_permlane16_swap(u, v, false, false);
+      a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
+    }
+  };
+#pragma unroll
+  for (int e = 0; e < N; e += 2) {
+    swap(x[e], x[e + 1]);
+    const float s = x[e] + x[e + 1], d = x[e] - x[e + 1];
+    x[e] = s, x[e + 1] = d;
+    swap(x[e], x[e + 1]);
+  }
+}
+
 // Butterfly stages across the lanes of a wave (lane xor 1 ... 8, then 16 and 32 as far as stages,
 // 4 to 6, goes) on N registers a lane (N even). Strides 1 ... 8 take the partner by DPP and x = y -+ x in one FMA (exact); strides 16 and
 // 32 exchange rows between two registers, add and subtract them, and exchange back. No LDS
@@ -66,28 +89,10 @@ __device__ __forceinline__ void hadamard_lanes(float (&x)[N], int lane, int stag
     x[e] = fmaf(x[e], s2, dpp_mov<0x1B>(dpp_mov<0x141>(x[e])));  // half mirror, quad mirror
     x[e] = fmaf(x[e], s3, dpp_mov<0x128>(x[e]));                 // row_ror 8
   }
-  auto pair = [](float& a, float& b, auto swap) {
-    swap(a, b);
-    const float s = a + b, d = a - b;
-    a = s, b = d;
-    swap(a, b);
-  };
-  auto swap16 = [](float& a, float& b) {
-    const auto r =
-        __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-    a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
-  };
-  auto swap32 = [](float& a, float& b) {
-    const auto r =
-        __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-    a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
-  };
   if (stages < 5) return;
-#pragma unroll
-  for (int e = 0; e < N; e += 2) pair(x[e], x[e + 1], swap16);
+  stage_rows<N, false>(x);
   if (stages < 6) return;
-#pragma unroll
-  for (int e = 0; e < N; e += 2) pair(x[e], x[e + 1], swap32);
+  stage_rows<N, true>(x);
 }
 
 // One group of up to 3 butterfly stages (strides h, 2h, 4h; h = 2^lgh) over a buffer of n

@@ -29,6 +29,10 @@ __device__ __forceinline__ uint16_t f32_bf16(float v) {
   return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
 }
 
+// The chunk of 8 channels that lane n of each 16 holds: the chunk 4 further on is the mirrored lane of
+// 8, so that every stage between chunks is one multiply-add.
+__device__ __forceinline__ int chunk_of(int n) { return n ^ ((n & 4) ? 3 : 0); }
+
 // ---- append --------------------------------------------------------------------------------------
 struct AppendArgs {
   const void *k, *v;
@@ -120,7 +124,7 @@ template <typename T, int DIM>
 __global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
   constexpr int LPR = DIM / 8, RPW = 256 / LPR;  // lanes per row, rows per workgroup
   const int l = threadIdx.x % LPR;
-  const int chunk = l ^ ((l & 4) ? 3 : 0);  // (the chunk 4 further on is the mirrored lane of 8)
+  const int chunk = chunk_of(l);
   const int64_t row = int64_t(blockIdx.x) * RPW + threadIdx.x / LPR;  // token, head, key or value
   const int64_t rows = A.n_tokens * A.n_kv * 2;
   if (row >= rows) return;  // (whole groups of LPR lanes)
@@ -254,6 +258,7 @@ struct AttnArgs {
   int tiles, splits;
   uint16_t* out;
   int64_t ldo;
+  bool wide;          // 16-byte stores of outputs
   float *part, *ml;   // splits > 1: [split][token][head][dim], and maximum and sum
 };
 
@@ -276,21 +281,6 @@ __device__ __forceinline__ void store_row(uint16_t* o, float (&x)[2], int lane, 
   if constexpr (DIM == 128) o[lane + 64] = f32_bf16(x[1]);
 }
 
-// the butterfly stages over lanes 0 to 15 (of each 16): channels 8 n + d of row_dim 128 and, with
-// n & 7 and 4 (n >> 3) + d, of 64
-template <int ND>
-__device__ __forceinline__ void turn16(float (&x)[ND], int n) {
-  const float s0 = (n & 1) ? -1.f : 1.f, s1 = (n & 2) ? -1.f : 1.f;
-  const float s2 = (n & 4) ? -1.f : 1.f, s3 = (n & 8) ? -1.f : 1.f;
-#pragma unroll
-  for (int e = 0; e < ND; ++e) {
-    x[e] = fmaf(x[e], s0, dpp_mov<0xB1>(x[e]));
-    x[e] = fmaf(x[e], s1, dpp_mov<0x4E>(x[e]));
-    x[e] = fmaf(x[e], s2, dpp_mov<0x1B>(dpp_mov<0x141>(x[e])));
-    x[e] = fmaf(x[e], s3, dpp_mov<0x128>(x[e]));
-  }
-}
-
 __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a),
                                                 __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
@@ -308,6 +298,7 @@ __device__ __forceinline__ void wait_vm() {  // s_waitcnt vmcnt(N), the other co
 // a second tile left one wave less per SIMD and a single tile of each wave on its way (156 us where it
 // takes 129, 48 sequences of up to 16384 tokens).
 constexpr int DEPTH = 4;
+constexpr float NONE = -1e30f;
 constexpr int tile_words(int dim) { return 2 * (64 * (dim / 32) + 256 + 64); }
 
 template <int DIM, int MQ, bool BY_ROWS>
@@ -324,8 +315,8 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g4 = lane >> 4;
-  const int b = blockIdx.z, h = blockIdx.y;
-  const int split = blockIdx.x % A.splits;
+  const int b = blockIdx.y, h = blockIdx.x;
+  const int split = blockIdx.z % A.splits;
   const int nt = int(A.n_tokens);
   int q0 = b, q1 = b + 1;
   if (A.starts) {
@@ -340,9 +331,10 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
   len = len < 0 ? 0 : len > most ? most : len;
   const int* table = A.table + int64_t(b) * A.ldt;
   const int page_mask = (1 << A.page_log) - 1;
-  // later rows see more tokens: they go first
+  // later rows see more tokens: they go first, of all sequences (by sequences, the last ones of a long
+  // sequence late in the grid ran alone at the end: 244 us for prompts of 2048 to 274 tokens)
   const int tiles = (nrows + TILE - 1) / TILE;
-  for (int tile = tiles - 1 - int(blockIdx.x / A.splits); tile >= 0; tile -= A.tiles) {
+  for (int tile = tiles - 1 - int(blockIdx.z / A.splits); tile >= 0; tile -= A.tiles) {
     const int row0 = tile * TILE + (BY_ROWS ? wave * ROWS : 0);
     if (BY_ROWS && row0 >= nrows) continue;
     const int end_row = row0 + ROWS < nrows ? row0 + ROWS : nrows;
@@ -375,13 +367,8 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
       }
       if (A.rotate) {
         hadamard_reg<8 * NJ>(x);
-#pragma unroll
-        for (int o = 16; o < 64; o <<= 1)
-#pragma unroll
-          for (int k = 0; k < 8 * NJ; ++k) {
-            const float p = __shfl_xor(x[k], o);
-            x[k] = (lane & o) ? p - x[k] : x[k] + p;
-          }
+        stage_rows<8 * NJ, false>(x);
+        stage_rows<8 * NJ, true>(x);
       }
       float mx = 0.f;
 #pragma unroll
@@ -414,16 +401,18 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
     }
 
     f32x4_t acc[MQ][ND] = {};
-    float m[MQ], l[MQ], zs[MQ], sigma = 0.f, sinv = 0.f;
+    // the reference m of a row (NONE: it has seen no token), what is subtracted from its scores, and
+    // how far above it they may be
+    float m[MQ], ref[MQ], above[MQ], l[MQ], zs[MQ], sigma = 0.f, sinv = 0.f;
 #pragma unroll
-    for (int i = 0; i < MQ; ++i) m[i] = -1e30f, l[i] = 0.f, zs[i] = 0.f;
+    for (int i = 0; i < MQ; ++i) m[i] = NONE, ref[i] = 0.f, above[i] = -INFINITY, l[i] = zs[i] = 0.f;
 
     // The pages of this wave's next 32 tiles, one of their halves of 16 a lane: read one by one, each
     // tile would wait for its page before it could ask for its codes. Tokens past the end: the last
     // ones again, masked below.
     const int first = beg_t + (BY_ROWS ? 0 : 32 * wave);
     int pages = 0, k0 = -32;
-    const unsigned at_k = (n * WPR + g4 * NJ) * 4, at_v = (g4 * WPR + (n & (WPR - 1))) * 16;
+    const unsigned at_k = (n * WPR + g4 * NJ) * 4, at_v = (g4 * WPR + chunk_of(n & (WPR - 1))) * 16;
     const unsigned at_p = (n + ((lane & 16) << A.page_log >> 4)) * 4;  // keys, then values
     uint32_t* const ring = reinterpret_cast<uint32_t*>(sm) + wave * DEPTH * TW;
     auto token = [&](int t) { return t < end ? t : (end - 1) & ~15; };
@@ -520,14 +509,14 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
           const float ks = __uint_as_float(T.kp[f][r] & 0xFFFF0000u), kz = float(T.kp[f][r] & 0xFFu);
 #pragma unroll
           for (int i = 0; i < MQ; ++i) {
-            float v = fmaf(-kz, qsum[i], s[i][f][r]) * (ks * qs[i]);
+            float v = fmaf(fmaf(-kz, qsum[i], s[i][f][r]), ks * qs[i], -ref[i]);
             if (CUT && (t0 + 16 * f + 4 * g4 + r >= see[i] || !counts(f, r))) v = -INFINITY;
             s[i][f][r] = v;
             top[i] = fmaxf(top[i], v);
           }
         }
 #pragma unroll
-      for (int i = 0; i < MQ; ++i) up |= top[i] > m[i] + 7.f;
+      for (int i = 0; i < MQ; ++i) up |= top[i] > above[i];
       if (__any(up)) {  // new references
         float sn = svm;
 #pragma unroll
@@ -540,7 +529,14 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
         for (int i = 0; i < MQ; ++i) {
           float t = fmaxf(top[i], __shfl_xor(top[i], 16));
           t = fmaxf(t, __shfl_xor(t, 32));
-          const float mn = fmaxf(m[i], t), fm = exp2f(m[i] - mn), fo = fm * fs;
+          const float mn = fmaxf(m[i], ref[i] + t), fm = exp2f(m[i] - mn), fo = fm * fs;
+          if (mn > NONE) {
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) s[i][f][r] += ref[i] - mn;
+            ref[i] = mn, above[i] = 7.f;
+          }
           m[i] = mn;
           l[i] *= fm, zs[i] *= fo;
           float fr[4];
@@ -568,8 +564,8 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
           const float z0 = float(T.vp[f][r] & 0xFFu), z1 = float(T.vp[f][r + 1] & 0xFFu);
 #pragma unroll
           for (int i = 0; i < MQ; ++i) {
-            const float p0 = __builtin_amdgcn_exp2f(s[i][f][r] - m[i]);
-            const float p1 = __builtin_amdgcn_exp2f(s[i][f][r + 1] - m[i]);
+            const float p0 = __builtin_amdgcn_exp2f(s[i][f][r]);
+            const float p1 = __builtin_amdgcn_exp2f(s[i][f][r + 1]);
             l[i] += p0 + p1;
             float w0 = p0 * s0, w1 = p1 * s1;
             if (CUT) {  // a hidden token's value may read as NaN
@@ -621,17 +617,20 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
     // this wave's tiles
     if (count > 0) {
       for (int k = 0; k < DEPTH - 1; ++k) load(k);
-      for (int k = 0; k < count; ++k) {
+      auto next = [&](int k, auto cut_c) {
+        const unsigned off = bad >> (2 * (k & (DEPTH - 1))) & 3;
         load(k + DEPTH - 1);  // (to the place of the tile before this one, which has been read)
         wait_vm<(DEPTH - 1) * LOADS>();
         __builtin_amdgcn_sched_barrier(0);
-        const int t0 = first + STEP * k;
-        const unsigned off = bad >> (2 * (k & (DEPTH - 1))) & 3;
-        if (t0 + 32 > end_t || t0 + 32 > see0 || off)
-          work(k, t0, off, std::true_type{});
-        else
-          work(k, t0, off, std::false_type{});
-      }
+        work(k, first + STEP * k, off, cut_c);
+      };
+      // whole tiles first, the rest (all of it from a page on that does not exist) in a loop of its own:
+      // two bodies in one loop hold their sums in different registers, and copy them
+      const int whole = end_t < see0 ? end_t : see0;
+      int k = 0;
+      for (; k < count && first + STEP * k + 32 <= whole && !(bad >> (2 * (k & (DEPTH - 1))) & 3); ++k)
+        next(k, std::false_type{});
+      for (; k < count; ++k) next(k, std::true_type{});
       wait_vm<0>();  // (loads past the end)
     }
 #pragma unroll
@@ -642,42 +641,73 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
       zs[i] += __shfl_xor(zs[i], 32);
     }
     // channel of block d of this lane
-    auto channel = [&](int d) { return DIM == 128 ? 8 * n + d : 8 * (n & 7) + 4 * (n >> 3) + d; };
+    const int chunk16 = chunk_of(n);
+    auto channel = [&](int d) {
+      return DIM == 128 ? 8 * chunk16 + d : 8 * (chunk16 & 7) + 4 * (n >> 3) + d;
+    };
 
     if constexpr (BY_ROWS) {
+      constexpr int RR = 8 / ND;  // rows at a time: eight registers for the stages between lanes
+      const bool alone = A.splits == 1;
+      const float norm = DIM == 128 ? 0.08838834764831845f : 0.125f;
+      const float sign = (__popc(unsigned(chunk16)) & 1) ? -norm : norm;
 #pragma unroll
       for (int i = 0; i < MQ; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = row0 + 16 * i + 4 * g4 + r;
-          const float z = __shfl(zs[i], 4 * g4 + r), sum = __shfl(l[i], 4 * g4 + r);
-          const float mm = __shfl(m[i], 4 * g4 + r);
-          const bool whole = A.splits == 1;
-          const float f = !whole ? sigma : sum == 0.f ? 0.f : sigma / sum;  // (sees nothing: zeros)
-          float o[ND];
+        for (int r0 = 0; r0 < 4; r0 += RR) {
+          float o[8], mm[RR], sum[RR];
 #pragma unroll
-          for (int d = 0; d < ND; ++d) o[d] = f * (acc[i][d][r] * (d & 1 ? 0x1p20f : 0x1p24f) - z);
-          if (whole && A.rotate) {
-            hadamard_reg<ND>(o);
-            turn16<ND>(o, n);
-            const float norm = DIM == 128 ? 0.08838834764831845f : 0.125f;
+          for (int u = 0; u < RR; ++u) {
+            const int r = r0 + u;
+            const float z = __shfl(zs[i], 4 * g4 + r);
+            sum[u] = __shfl(l[i], 4 * g4 + r), mm[u] = __shfl(m[i], 4 * g4 + r);
+            // (a row that sees nothing: zeros)
+            const float f = !alone ? sigma : sum[u] == 0.f ? 0.f : sigma / sum[u];
+            float x[ND];
 #pragma unroll
-            for (int d = 0; d < ND; ++d) o[d] *= norm;
+            for (int d = 0; d < ND; ++d) x[d] = f * (acc[i][d][r] * (d & 1 ? 0x1p20f : 0x1p24f) - z);
+            if (alone && A.rotate) hadamard_reg<ND>(x);
+#pragma unroll
+            for (int d = 0; d < ND; ++d) o[ND * u + d] = x[d];
           }
-          if (row >= nrows) continue;
-          const int64_t tok = q0 + row / G;
-          const int head = h * G + row % G;
-          if (whole) {
-            uint16_t* out = A.out + tok * A.ldo + int64_t(head) * DIM + channel(0);
+          if (alone && A.rotate) {
+            stage_lane1(o, (chunk16 & 1) ? -1.f : 1.f);
+            stage_lane2(o, (chunk16 & 2) ? -1.f : 1.f);
+            stage_mirror8(o, (chunk16 & 4) ? -1.f : 1.f);
+            stage_lane8(o, (chunk16 & 8) ? -1.f : 1.f);
 #pragma unroll
-            for (int d = 0; d < ND; ++d) out[d] = f32_bf16(o[d]);
-          } else {
-            const int64_t at = (int64_t(split) * A.n_tokens + tok) * A.n_heads + head;
+            for (int d = 0; d < 8; ++d) o[d] *= sign;
+          }
 #pragma unroll
-            for (int d = 0; d < ND; d += 4)
-              *reinterpret_cast<f32x4_t*>(A.part + at * DIM + channel(d)) =
-                  f32x4_t{o[d], o[d + 1], o[d + 2], o[d + 3]};
-            if (n == 0) A.ml[2 * at] = mm, A.ml[2 * at + 1] = sum;
+          for (int u = 0; u < RR; ++u) {
+            const int row = row0 + 16 * i + 4 * g4 + r0 + u;
+            if (row >= nrows) continue;
+            const int64_t tok = q0 + row / G;
+            const int head = h * G + row % G;
+            const float* const x = o + ND * u;
+            if (!alone) {
+              const int64_t at = (int64_t(split) * A.n_tokens + tok) * A.n_heads + head;
+#pragma unroll
+              for (int d = 0; d < ND; d += 4)
+                *reinterpret_cast<f32x4_t*>(A.part + at * DIM + channel(d)) =
+                    f32x4_t{x[d], x[d + 1], x[d + 2], x[d + 3]};
+              if (n == 0) A.ml[2 * at] = mm[u], A.ml[2 * at + 1] = sum[u];
+              continue;
+            }
+            uint16_t* const out = A.out + tok * A.ldo + int64_t(head) * DIM + channel(0);
+            if (A.wide) {
+              uint32_t w[ND / 2];
+#pragma unroll
+              for (int d = 0; d < ND; d += 2)
+                w[d / 2] = uint32_t(f32_bf16(x[d])) | uint32_t(f32_bf16(x[d + 1])) << 16;
+              if constexpr (ND == 8)
+                *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+              else
+                *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+            } else {
+#pragma unroll
+              for (int d = 0; d < ND; ++d) out[d] = f32_bf16(x[d]);
+            }
           }
         }
       continue;
@@ -771,8 +801,8 @@ int launch_attention(const AttnArgs& a, int64_t n_seqs, hipStream_t s) {
   const size_t tiles = size_t(4) * DEPTH * tile_words(DIM) * 4;
   const size_t ends = BY_ROWS ? 0 : size_t(4) * 16 * MQ * (DIM + 4 + 2) * sizeof(float);
   const size_t lds = tiles > ends ? tiles : ends;
-  const dim3 grid(static_cast<unsigned>(a.tiles * a.splits), static_cast<unsigned>(a.n_kv),
-                  static_cast<unsigned>(n_seqs));
+  const dim3 grid(static_cast<unsigned>(a.n_kv), static_cast<unsigned>(n_seqs),
+                  static_cast<unsigned>(a.tiles * a.splits));
   KQ_TRY(launch("cache_attention", cache_attention<DIM, MQ, BY_ROWS>, grid, dim3(256), lds, s, a));
   if (a.splits == 1) return KRONQ_OK;
   return launch("attention_join", attention_join<DIM>,
@@ -812,6 +842,7 @@ int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {
   a.table = j.table, a.ldt = j.ldt, a.table_pages = int(j.table_pages), a.lengths = j.lengths;
   a.starts = j.starts, a.scale = j.scale * 1.4426950408889634f, a.rotate = j.rotate;
   a.out = static_cast<uint16_t*>(j.out), a.ldo = j.ldo;
+  a.wide = aligned(j.out, 16) && j.ldo % 8 == 0;
   // Up to 64 rows of a sequence and kv head share their tokens out to the waves (two tiles of 32 rows
   // from 33 on); more are walked by 128 rows a workgroup, which read the tokens once for all of them.
   const int64_t rows = j.max_new * a.group;
@@ -826,6 +857,8 @@ int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {
   splits = splits < MAX_SPLITS ? splits : MAX_SPLITS;
   if (splits * all > split_rows(all)) splits = split_rows(all) / all;
   a.splits = int(splits < 1 ? 1 : splits);
+  // (the last dimension of the grid: more tiles are walked in turn)
+  a.tiles = a.tiles * a.splits <= 65535 ? a.tiles : 65535 / a.splits;
   Carver cv(ws);
   const size_t cap = size_t(split_rows(all));
   a.part = cv.take<float>(cap * size_t(j.dim));
