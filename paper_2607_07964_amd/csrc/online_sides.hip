@@ -568,19 +568,37 @@ struct Products {
       for (int k = 0; k < 8; ++k) v[k] *= w[k];
     }
   }
-  __device__ __forceinline__ float sum1(int j) const {
-    float v = float(p[j]);
-    if (A.workers == 0) return v;
-    int from, to;
-    parts(j, from, to);
-    for (; from < to; from += 4) {
-      float u[4];
+  // elements j + k step below d, their parts four at a time and all of them together: one after another
+  // they wait for memory as often as there are parts
+  template <int K>
+  __device__ __forceinline__ void sum_each(int j, int step, int d, float (&v)[K]) const {
+    int from[K], to[K], most = 0, at[K];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) u[i] = float(*kept(from + i < to ? from + i : to - 1, j));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v += from + i < to ? u[i] : 0.f;
+    for (int k = 0; k < K; ++k) {
+      at[k] = j + k * step < d ? j + k * step : j;
+      v[k] = float(p[at[k]]);
+      from[k] = to[k] = 0;
+      if (A.workers) parts(at[k], from[k], to[k]);
+      most = max(most, to[k] - from[k]);
     }
-    return w_unit ? v * w_unit[j] : v;
+    for (int s = 0; s < most; s += 4) {
+      float u[K][4];
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int w = from[k] + s + i;
+          u[k][i] = to[k] > from[k] ? float(*kept(w < to[k] ? w : to[k] - 1, at[k])) : 0.f;
+        }
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[k] += from[k] + s + i < to[k] ? u[k][i] : 0.f;
+    }
+    if (w_unit) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] *= w_unit[at[k]];
+    }
   }
 };
 
@@ -780,12 +798,21 @@ __global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
   const T* const res = A.residual ? static_cast<const T*>(A.residual) + row * A.ldr : nullptr;
   T* const y = static_cast<T*>(A.y) + row * A.ldy;
   const Products<TP> products(A, row, expert);
-  for (int j = tid; j < d; j += 256) {
-    const float v = products.sum1(j);
-    if (A.turn.rotate)
-      small[j] = v;  // (d <= 28 * 4)
-    else
-      store1<T>(y, j, finish<T>(v * up, j, mul, bias, res, A.act));
+  constexpr int K = 4;
+  for (int j = tid; j < d; j += 256 * K) {
+    float v[K];
+    products.template sum_each<K>(j, 256, d, v);
+    if (A.turn.rotate) {
+      small[j] = v[0];  // (d <= 28 * 4)
+      break;
+    }
+#pragma unroll 1
+    for (int k = 0; k < K; ++k) {
+      const int at = j + 256 * k;
+      if (at < d) store1<T>(y, at, finish<T>(v[0] * up, at, mul, bias, res, A.act));
+#pragma unroll
+      for (int i = 1; i < K; ++i) v[i - 1] = v[i];
+    }
   }
   if (!A.turn.rotate) return;
   __syncthreads();
