@@ -7,8 +7,9 @@
 //   1. linear_in: x' as fp16 in MFMA-fragment order, each row scaled by a power of two of its own
 //      that brings its largest value into [2^7, 2^8); beside it the tables of the weights' scales
 //      and zeros, and for experts the list of row tiles.
-//   2. linear_ring: products of 32 rows and 32 rows of W_hat' on v_mfma_f32_32x32x16_f16. A lane
-//      reads the packed codes of its own weight row and spreads them to fp16 in registers.
+//   2. linear_few or, for many rows, linear_ring: products of 32 rows and 32 rows of W_hat' on
+//      v_mfma_f32_32x32x16_f16. A lane takes the packed codes of its own weight row and spreads them
+//      to fp16 in registers.
 //   3. linear_out: the transform of y', and the epilogue.
 // Weights enter the matrix products in one of two forms (SCALED below): as fp16 s (c - z), each row
 // of W divided by a power of two, from a table of fp16 scales and offsets that linear_in prepares
@@ -173,7 +174,7 @@ __device__ __forceinline__ void load_codes(uint32_t* w, const uint32_t* p) {
 // rows of W (32 a wave) and a tile of NT units; everything comes straight to LDS in whole lines, and
 // the lanes take their own rows' codes from there. (Codes that each lane loads from its own row are
 // one L1 access a lane: those bound it, 66 us for 8 experts of 14336 x 4096 at 4 bits with 32 rows
-// that take FEW_US now.) In LDS:
+// that take 52 this way, at 3.3 TB/s of what has to be read.) In LDS:
 //   x': RG groups of NP pieces (unit, plane) of 8 KB in fragment order, one step of 16 columns a wave;
 //   codes: CB batches of BG groups, of LB bytes a row: with rows of 128 bytes piece p of 16 stands at
 //     p ^ (row & 7), so that eight lanes reading theirs meet in no bank;
@@ -395,7 +396,7 @@ __global__ __launch_bounds__(512, 2) void linear_few(MmArgs A) {
   }
 }
 
-// A workgroup of four waves takes 128 RT rows of W (32 RT a wave) and a tile of NT units of rows of
+// Many rows. A workgroup of four waves takes 128 RT rows of W (32 RT a wave) and a tile of NT units of rows of
 // x'; a lane holds the codes of RT rows of W and half of the columns, 64 of them a stage. x' comes
 // through LDS: a stage is 64 columns (half a group, a chunk of each lane's codes) of NT units in
 // PLANES planes, pieces of 4 KB that the waves bring straight to LDS, in fragment order as they
@@ -407,12 +408,9 @@ __global__ __launch_bounds__(512, 2) void linear_few(MmArgs A) {
 //     other's matrix instructions. Results leave as fp16 (linear_out multiplies by the units of the
 //     rows of W).
 //   PLANES = 2, NT = 2, RT = 2: the same for fp32 results.
-//   RT = 1 (few rows): the codes' way from memory bounds it, with three or four workgroups per CU.
-// A lane reads its row of W in batches, of a whole 128-byte line with RT = 1: chunk by chunk the lines
-// left the L1 between two reads of one, and came from L2 up to four times. The fp32 scales and zeros
-// (not SCALED) come through LDS eight groups at a time for the same reason: 32 rows lie in 32 lines of
-// either. (8 experts of 14336 x
-// 4096 at 4 bits with 32 rows: 76 us that way, 66 now.)
+// 8192 rows of 4096 x 4096 at 4 bits: 240 us, 1.15 PFLOP/s, where a large plain matrix product reaches
+// 1.22 to 1.32. A lane reads its row of W in batches; the fp32 scales and zeros (not SCALED) come
+// through LDS eight groups at a time, since 32 rows lie in 32 lines of either.
 template <int BITS, int NT, int PLANES, bool SCALED>
 __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
   constexpr int RT = BLOCK / 128;                        // units of 32 rows of W a wave
@@ -664,10 +662,13 @@ struct Plan {
 Plan make_plan(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts, int y_dtype) {
   Plan p;
   p.planes = y_dtype == KRONQ_BF16 ? 1 : 2;
-  // A tile of 32 rows for up to 32 rows (of an expert), of 64 up to 64; more rows share the spread
-  // codes best in tiles of 128 (64 in two planes).
+  // A tile of 32 rows for up to 32 rows (of an expert); more rows share the spread codes in tiles of
+  // 64, or of 128 with the table, which pays for itself late: one layer at 4 bits takes, in tiles of
+  // 64 and of 128, 36 and 43 us for 256 rows of 4096 x 4096, 71 and 72 us for 256 rows of 14336 x
+  // 4096, 125 and 106 us for 512 of these; 8 experts of 14336 x 4096 take 169 and 163 us for 64 rows
+  // each, 207 and 178 us for 80 each.
   const int64_t rows = cdiv(n_rows, n_experts);
-  p.scaled = p.planes == 1 && rows > 64;
+  p.scaled = p.planes == 1 && rows > (n_experts == 1 ? 256 : 64);
   p.nt = p.scaled ? 4 : rows > 32 ? 2 : 1;
   p.few = p.nt * p.planes < 4;
   p.tiles = n_experts == 1 ? cdiv(n_rows, 32 * p.nt) : most_tiles(n_rows, n_experts, p.nt);

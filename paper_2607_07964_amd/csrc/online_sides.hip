@@ -699,9 +699,10 @@ __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
 }
 
 // A few rows of 28 m: four workgroups to a row, 7 segments each, where one to a row would leave most
-// CUs idle (a row of 14336 is 16 us of work for one). Each sums all products of the row, so the factor
-// comes first here: 16 x 16 tiles of it on the matrix cores take a workgroup's 7 rows of the factor
-// (PARTS_FIGURE).
+// CUs idle. Each sums all products of the row, so the factor comes first here: 16 x 16 tiles of it on
+// the matrix cores take a workgroup's 7 rows of the factor. Rows of 14336: 16 of them 11.0 us, where
+// one workgroup each takes 14.5; 32 of them 12.4 and 14.5; 64 of them 17.5 and 14.8, so that half of
+// the CUs is the limit.
 constexpr int PARTS = 4;
 template <typename TP, typename T, int B>
 __global__ __launch_bounds__(1024) void linear_out_part(LinearOut A) {
@@ -877,7 +878,7 @@ int out_typed(LinearOut a, hipStream_t s) {
     return launch("linear_out", linear_out_any<TP, T>, grid, dim3(256), 0, s, a);
 #define KQ_OUT(C_, F_) \
   launch("linear_out", linear_out<TP, T, C_, F_>, grid, dim3(threads(C_)), size_t(a.d_out) * 4, s, a)
-  if (a.turn.has28 && a.n_rows * PARTS <= device_cus()) {
+  if (a.turn.has28 && a.n_rows * PARTS <= device_cus() / 2) {
     const dim3 parts(static_cast<unsigned>(a.n_rows * PARTS));
     return a.turn.m == 1024
                ? launch("linear_out", linear_out_part<TP, T, 2>, parts, dim3(1024),
