@@ -208,3 +208,10 @@ def test_causal_attention_by_hand():
     # shared heads
     o2 = O.causal_attention(np.repeat(q, 2, 1), k, v, 1.0)
     np.testing.assert_allclose(o2[:, 0], o2[:, 1])
+
+
+@pytest.mark.parametrize("change", [dict(ldp=(1 << 20) + 4), dict(ldsz=(1 << 20) + 1)])
+def test_linear_refuses_rows_of_weights_too_far_apart(change):
+    """(256 rows of W are addressed with 32-bit offsets)"""
+    rc, msg = linear(**change)
+    assert rc == -6 and "2^20" in msg, (rc, msg)
