@@ -323,7 +323,9 @@ __global__ __launch_bounds__(512, 2) void linear_few(MmArgs A) {
           __builtin_amdgcn_s_barrier();
           asm volatile("" ::: "memory");
           issue_x(g + RG - 1);
+          __builtin_amdgcn_sched_barrier(0);  // (the order that `newer` counts on)
           if constexpr (u == 0) issue_codes(g / BG + CB - 1);
+          __builtin_amdgcn_sched_barrier(0);
           if ((g & 3) == 0) issue_params(g + 4);
           __builtin_amdgcn_sched_barrier(0);
           read_codes(cw1, g + 1, std::integral_constant<int, (u + 1) % BG>{});
@@ -353,6 +355,7 @@ __global__ __launch_bounds__(512, 2) void linear_few(MmArgs A) {
 #pragma unroll
     for (int s = -FIRST; s < 0; ++s) {
       if (s + RG - 1 >= 0) issue_x(s + RG - 1);
+      __builtin_amdgcn_sched_barrier(0);
       if (s % BG == 0) issue_codes(s / BG + CB - 1);
       __builtin_amdgcn_sched_barrier(0);
     }

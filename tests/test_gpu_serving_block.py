@@ -221,3 +221,47 @@ def test_append_rows_next_to_the_borders_of_the_grid(rotate, dim):
     for hat, t in zip(hats, (k, -k)):
         q, scale, zero, held = O.cache_grid(f64(t), rotate)
         assert np.array_equal(f64(hat), held.astype(np.float32).astype(np.float64))
+
+
+@pytest.mark.parametrize("rows,first,last", [(260, 10, 200), (700, 33, 700), (9, 0, 9)])
+def test_one_expert_of_some_rows(rows, first, last):
+    """A single expert that begins inside a unit of 32 rows; the other rows keep what they hold."""
+    la = Layer(256, 512, 4, 128, BOTH, seed=12)
+    x = rows_of(rows, 512, BF16, seed=13)
+    y = torch.full((rows, 256), 7.0, dtype=BF16, device=DEV)
+    offsets = torch.tensor([first, last], dtype=torch.int32, device=DEV)
+    note(f"one expert rows={rows} [{first}, {last})")
+    K.kronq_online_grouped(*la.args, *la.factors, x.to(DEV), offsets, y, bias=la.bias_d, flags=BOTH)
+    torch.cuda.synchronize()
+    assert rel_frob(f64(y)[first:last], la.ref(f64(x)[first:last])) < TOL[BF16]
+    assert bool((y[:first] == 7).all()) and bool((y[last:] == 7).all())
+
+
+@pytest.mark.parametrize("d_out,rows", [(224, 5), (224, 33), (28672, 32), (28672, 33), (896, 6)])
+@pytest.mark.parametrize("ydt", [BF16, torch.float32])
+def test_outputs_of_28_m_by_one_and_by_four_workgroups(d_out, rows, ydt):
+    """Both ways of the output side, with every part of its epilogue."""
+    la = Layer(d_out, 256, 4, 128, BOTH, seed=14)
+    x, res = rows_of(rows, 256, BF16, seed=15), rows_of(rows, d_out, ydt, seed=16)
+    note(f"28 m outputs d_out={d_out} rows={rows} {ydt}")
+    y = K.kronq_online_linear(*la.one(), x.to(DEV), bias=la.bias_d[0], act="gelu",
+                              residual=res.to(DEV), out_dtype=ydt)
+    torch.cuda.synchronize()
+    assert rel_frob(f64(y), la.ref(f64(x), "gelu", f64(res))) < TOL[ydt]
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4, 8])
+@pytest.mark.parametrize("groups", [1, 2, 3, 5, 9])
+@pytest.mark.parametrize("ydt", [BF16, torch.float32])
+def test_few_rows_and_few_groups(bits, groups, ydt):
+    """Rows of W of few groups, whose loads end in any place of the rings; wide strides of W."""
+    la = Layer(300, 128 * groups, bits, 128, 0, seed=17)
+    x = rows_of(20, 128 * groups, BF16, seed=18)
+    wide = torch.full((300, la.packed.shape[1] + 4), -1, dtype=torch.int32, device=DEV)
+    wide[:, :la.packed.shape[1]] = la.packed.view(torch.int32)
+    note(f"few groups bits={bits} groups={groups} {ydt}")
+    for packed in (la.packed, wide[:, :la.packed.shape[1]]):
+        y = K.kronq_online_linear(packed, *la.one()[1:], x.to(DEV), bias=la.bias_d[0], flags=0,
+                                  out_dtype=ydt)
+        torch.cuda.synchronize()
+        assert rel_frob(f64(y), la.ref(f64(x))) < TOL[ydt]
