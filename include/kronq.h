@@ -433,7 +433,7 @@ int kronq_cache_append(const void* k, const void* v, int dtype, int64_t ldk, int
  * last ones of sequence b, whose lengths[b] cached tokens include them: its i-th of n new tokens
  * sees cached tokens 0 to lengths[b] - n + i. A token that sees none gets zeros.
  *   q, out   device bf16 [n_tokens][n_heads][dim], tokens ldq / ldo elements apart; q 16-byte
- *            aligned with ldq divisible by 8, out 2-byte aligned.
+ *            aligned with ldq divisible by 8, out 2-byte aligned, not overlapping q.
  *   table    device int32 [n_seqs x ldt]: the page of tokens j * page to j * page + page - 1 of
  *            sequence b in column j, table_pages columns. Tokens on a page outside [0, n_pages)
  *            are not seen.
