@@ -426,6 +426,9 @@ int kronq_cache_append(const void* k, const void* v, int dtype, int64_t ldk, int
                        uint32_t* codes, uint32_t* params, int64_t n_pages, int64_t page,
                        int rotate, float* k_hat, float* v_hat, void* stream);
 
+#define KRONQ_CACHE_ROTATE 1 /* keys and values were turned */
+#define KRONQ_CACHE_FILL 2   /* zeros for tokens of no sequence */
+
 /* Attention of new tokens over the cache, for decoding (one new token per sequence) and for
  * prompts packed one after another:
  *   out[t][h] = sum_s p_s V_s,  p = softmax over the visible s of scale * q[t][h] . K_s
@@ -440,19 +443,20 @@ int kronq_cache_append(const void* k, const void* v, int dtype, int64_t ldk, int
  *   lengths  device int32 [n_seqs]; cut to [0, table_pages * page].
  *   starts   device int32 [n_seqs + 1], ascending, cut to [0, n_tokens]; NULL: token b is the one
  *            new token of sequence b (n_tokens <= n_seqs). Tokens of no sequence keep what out
- *            holds.
+ *            holds, or get zeros with KRONQ_CACHE_FILL.
  *   max_new  host: at least one and about the largest number of new tokens of a sequence (it sizes
  *            the launch; a longer one is computed all the same, later).
  *   All of table, lengths and starts are read on the device, so that a captured call follows them.
  * Precision: rotated queries and the weights p (times the value's scale) in fp16, the latter not
  * coarser than 2^-25 of the largest value scale; sums in fp32.
- *   n_heads a multiple of n_kv; dim, page, rotate as in kronq_cache_append; n_seqs <= 65535,
+ *   flags   KRONQ_CACHE_ROTATE (as rotate of kronq_cache_append), KRONQ_CACHE_FILL.
+ *   n_heads a multiple of n_kv; dim, page as in kronq_cache_append; n_seqs <= 65535,
  *   n_kv <= 65535. n_tokens = 0 does nothing. Workspace: KRONQ_OP_ATTENTION. */
 int kronq_cache_attention(const void* q, int64_t ldq, int64_t n_tokens, int64_t n_heads,
                           int64_t n_kv, int64_t dim, const uint32_t* codes, const uint32_t* params,
                           int64_t n_pages, int64_t page, const int32_t* table, int64_t ldt,
                           int64_t table_pages, const int32_t* lengths, int64_t n_seqs,
-                          const int32_t* starts, int64_t max_new, float scale, int rotate,
+                          const int32_t* starts, int64_t max_new, float scale, int flags,
                           void* out, int64_t ldo, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- 8. diagnostics of the incoherence processing ------------------------------------------

@@ -215,7 +215,7 @@ struct AttentionJob {
   const int32_t* starts;
   int64_t max_new;
   float scale;
-  int rotate;
+  int flags;
   void* out;
   int64_t ldo;
 };

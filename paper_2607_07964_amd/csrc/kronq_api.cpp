@@ -625,10 +625,12 @@ int kronq_cache_attention(const void* q, int64_t ldq, int64_t n_tokens, int64_t 
                           int64_t n_kv, int64_t dim, const uint32_t* codes, const uint32_t* params,
                           int64_t n_pages, int64_t page, const int32_t* table, int64_t ldt,
                           int64_t table_pages, const int32_t* lengths, int64_t n_seqs,
-                          const int32_t* starts, int64_t max_new, float scale, int rotate,
+                          const int32_t* starts, int64_t max_new, float scale, int flags,
                           void* out, int64_t ldo, void* ws, size_t ws_bytes, void* stream) {
   kq::clear_error();
   KQ_TRY(check_cache(codes, params, n_pages, page, n_kv, dim));
+  KQ_REQUIRE((flags & ~(KRONQ_CACHE_ROTATE | KRONQ_CACHE_FILL)) == 0, KRONQ_ERR_INVALID_ARG,
+             "unknown flag bits 0x%x", flags & ~(KRONQ_CACHE_ROTATE | KRONQ_CACHE_FILL));
   KQ_REQUIRE(n_heads >= 1 && n_heads % n_kv == 0 && n_heads <= 65535, KRONQ_ERR_SHAPE,
              "n_heads must be a positive multiple of n_kv, at most 65535");
   KQ_REQUIRE(n_tokens >= 0 && n_tokens <= (int64_t(1) << 31) / (n_heads * 4),
@@ -653,7 +655,7 @@ int kronq_cache_attention(const void* q, int64_t ldq, int64_t n_tokens, int64_t 
   KQ_TRY(check_ws(ws, ws_bytes, kq::attention_ws_bytes(n_heads, dim, n_tokens)));
   const kq::AttentionJob j{q,      ldq,   n_tokens,    n_heads, n_kv,   dim,    codes,
                            params, n_pages, page,      table,   ldt,    table_pages, lengths,
-                           n_seqs, starts, max_new,    scale,   rotate != 0, out, ldo};
+                           n_seqs, starts, max_new,    scale,   flags,  out,    ldo};
   return kq::cache_attention_launch(j, ws, as_stream(stream));
 }
 

@@ -254,7 +254,7 @@ struct AttnArgs {
   const int* lengths;
   const int* starts;  // null: token b is sequence b
   float scale;        // of the scores, times log2(e)
-  int rotate;
+  int rotate, fill;
   int tiles, splits;
   uint16_t* out;
   int64_t ldo;
@@ -325,6 +325,15 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
     q1 = __builtin_amdgcn_readfirstlane(A.starts[b + 1]);
     q0 = q0 < 0 ? 0 : q0 > nt ? nt : q0;
     q1 = q1 < q0 ? q0 : q1 > nt ? nt : q1;
+    if (A.fill) {  // tokens before the first sequence and behind the last one, dealt to all workgroups
+      const int s0 = A.starts[0], s1 = A.starts[gridDim.y];
+      const int head = s0 < 0 ? 0 : s0 > nt ? nt : s0, tail = s1 < head ? head : s1 > nt ? nt : s1;
+      const int all = int(gridDim.y * gridDim.z), width = A.group * DIM;
+      for (int64_t k = b + int(gridDim.y * blockIdx.z); k < head + nt - tail; k += all) {
+        uint16_t* const out = A.out + (k < head ? k : k - head + tail) * A.ldo + int64_t(h) * width;
+        for (int e = tid; e < width; e += 256) out[e] = 0;
+      }
+    }
   }
   const int nq = q1 - q0, G = A.group, nrows = nq * G;
   int len = __builtin_amdgcn_readfirstlane(A.lengths[b]);
@@ -842,7 +851,8 @@ int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {
   a.codes = j.codes, a.params = j.params, a.n_pages = j.n_pages;
   a.page_log = __builtin_ctzll(uint64_t(j.page));
   a.table = j.table, a.ldt = j.ldt, a.table_pages = int(j.table_pages), a.lengths = j.lengths;
-  a.starts = j.starts, a.scale = j.scale * 1.4426950408889634f, a.rotate = j.rotate;
+  a.starts = j.starts, a.scale = j.scale * 1.4426950408889634f;
+  a.rotate = (j.flags & KRONQ_CACHE_ROTATE) != 0, a.fill = (j.flags & KRONQ_CACHE_FILL) != 0;
   a.out = static_cast<uint16_t*>(j.out), a.ldo = j.ldo;
   a.wide = aligned(j.out, 16) && j.ldo % 8 == 0;
   // Up to 64 rows of a sequence and kv head share their tokens out to the waves (two tiles of 32 rows

@@ -26,6 +26,7 @@ OP_COV, OP_ROTATE, OP_CHOL, OP_OBS, OP_LOSS = 1, 2, 3, 4, 5
 OP_CROSS, OP_ROTATE_DRIFT, OP_GPTAQ, OP_OBS_DRIFT, OP_ONLINE = 6, 7, 8, 9, 10
 OP_STATS, OP_EIGH, OP_PROXY, OP_COV_DIAG, OP_LINEAR, OP_ATTENTION = 11, 12, 13, 14, 15, 16
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+CACHE_FILL = 2
 MAX_ALPHAS = 16
 ERRORS = {0: "OK", -1: "INVALID_ARG", -2: "SHAPE", -3: "NOT_PD", -4: "HIP", -5: "WORKSPACE",
           -6: "UNSUPPORTED"}
@@ -428,12 +429,13 @@ def _same_device(*ts):
     for t in ts:
         if t is None:
             continue
-        if not t.is_cuda:
-            raise ValueError("libkronq works on device tensors only")
+        d = t.device
         if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device}")
+            dev = d
+            if d.type != "cuda":
+                raise ValueError("libkronq works on device tensors only")
+        elif d != dev:
+            raise ValueError(f"tensors on {dev} and {d}: device tensors of one device are needed")
     return dev
 
 
@@ -627,20 +629,23 @@ def kronq_cache_attention(q: torch.Tensor, codes: torch.Tensor, params: torch.Te
     """Attention of the new tokens q [tokens, heads, dim] (bf16) over the 4-bit cache. Tokens
     starts[b] to starts[b + 1] - 1 are the last of the lengths[b] cached tokens of sequence b (no
     starts: one each), whose pages table[b] names. ``max_new`` (default: all tokens, or 1 without
-    starts) is about the most new tokens of a sequence; ``scale`` defaults to dim ** -0.5."""
+    starts) is about the most new tokens of a sequence; ``scale`` defaults to dim ** -0.5. Tokens of
+    no sequence keep what out holds (zeros where out is made here)."""
     lib = load()
     dev = _same_device(q, codes, params, table, lengths, starts, out, ws)
     pages, kv, page, dim = _cache_sizes(codes, params)
-    n, heads = q.shape[0], q.shape[1]
+    n, heads = q.shape[:2]
     ldq = _token_stride(q, heads, dim, "q")
     if q.dtype != torch.bfloat16:
         raise ValueError("q must be bfloat16")
+    ldo, fill = heads * dim, 0
     if out is None:
-        out = torch.empty(n, heads, dim, dtype=torch.bfloat16, device=dev) if starts is None else \
-            torch.zeros(n, heads, dim, dtype=torch.bfloat16, device=dev)
-    if out.dtype != torch.bfloat16 or out.shape[0] != n:
+        out = torch.empty((n, heads, dim), dtype=torch.bfloat16, device=dev)
+        fill = CACHE_FILL
+    elif out.dtype != torch.bfloat16 or out.shape[0] != n:
         raise ValueError("out must be bfloat16 with q's shape")
-    ldo = _token_stride(out, heads, dim, "out")
+    else:
+        ldo = _token_stride(out, heads, dim, "out")
     seqs = table.shape[0]
     if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1
                                                          and table.stride(1) != 1):
@@ -650,7 +655,7 @@ def kronq_cache_attention(q: torch.Tensor, codes: torch.Tensor, params: torch.Te
     if starts is None and n != seqs:
         raise ValueError("without starts there is one token per sequence")
     if n == 0 or seqs == 0:
-        return out
+        return out.zero_() if fill else out
     most = max_new if max_new is not None else 1 if starts is None else n
     ldt = table.stride(0) if seqs > 1 else table.shape[1]
     with _guard(dev):
@@ -660,8 +665,8 @@ def kronq_cache_attention(q: torch.Tensor, codes: torch.Tensor, params: torch.Te
         rc = lib.kronq_cache_attention(
             q.data_ptr(), ldq, n, heads, kv, dim, codes.data_ptr(), params.data_ptr(), pages, page,
             table.data_ptr(), ldt, table.shape[1], lengths.data_ptr(), seqs, _addr(starts),
-            int(most), dim ** -0.5 if scale is None else float(scale), int(rotate), out.data_ptr(),
-            ldo, ws.data_ptr(), ws.numel() * ws.element_size(), _handle(dev))
+            int(most), dim ** -0.5 if scale is None else float(scale), int(bool(rotate)) | fill,
+            out.data_ptr(), ldo, ws.data_ptr(), ws.numel() * ws.element_size(), _handle(dev))
     _check(rc, "kronq_cache_attention")
     return out
 

@@ -265,3 +265,30 @@ def test_few_rows_and_few_groups(bits, groups, ydt):
                                   out_dtype=ydt)
         torch.cuda.synchronize()
         assert rel_frob(f64(y), la.ref(f64(x))) < TOL[ydt]
+
+
+@pytest.mark.parametrize("heads,dim,new,pad", [(4, 128, [1, 1, 1], 40), (8, 64, [90, 0, 40], 3),
+                                               (4, 128, [70], 0)])
+def test_attention_fills_tokens_of_no_sequence(heads, dim, new, pad):
+    """Zeros before the first and behind the last sequence where out is made by the call; with a given
+    out they stay as they are; the others are the same."""
+    n = sum(new) + 2 * pad
+    codes, params = K.kronq_cache_empty(8 * len(new), 1, dim, 16, DEV)
+    kv = torch.randn(2, 128 * len(new), 1, dim, generator=torch.Generator().manual_seed(5)).to(BF16)
+    K.kronq_cache_append(kv[0].to(DEV), kv[1].to(DEV), torch.arange(128 * len(new), device=DEV), codes,
+                         params)
+    table = torch.arange(8 * len(new), dtype=torch.int32, device=DEV).view(len(new), 8)
+    lengths = torch.full((len(new),), 100, dtype=torch.int32, device=DEV)
+    starts = torch.tensor(np.cumsum([pad] + new), dtype=torch.int32, device=DEV)
+    q = torch.randn(n, heads, dim, generator=torch.Generator().manual_seed(6)).to(BF16).to(DEV)
+    note(f"attention fills new={new} pad={pad}")
+    junk = torch.full((n, heads, dim), float("nan"), dtype=BF16, device=DEV)
+    del junk  # (what the allocator hands out next is not zero)
+    a = K.kronq_cache_attention(q, codes, params, table, lengths, starts=starts, max_new=max(new))
+    given = torch.full((n, heads, dim), 3.0, dtype=BF16, device=DEV)
+    K.kronq_cache_attention(q, codes, params, table, lengths, starts=starts, max_new=max(new), out=given)
+    torch.cuda.synchronize()
+    own = slice(pad, n - pad)
+    assert torch.equal(a[own], given[own]) and bool(a[own].any())
+    for cut in (slice(0, pad), slice(n - pad, n)):
+        assert not bool(a[cut].any()) and bool((given[cut] == 3).all())

@@ -215,3 +215,9 @@ def test_linear_refuses_rows_of_weights_too_far_apart(change):
     """(256 rows of W are addressed with 32-bit offsets)"""
     rc, msg = linear(**change)
     assert rc == -6 and "2^20" in msg, (rc, msg)
+
+
+def test_attention_refuses_unknown_flags():
+    lib = K.load()
+    rc = lib.kronq_cache_attention(*{**ATTEND, "rotate": 4}.values())
+    assert rc == -1 and "flag" in lib.kronq_last_error().decode()
