@@ -865,7 +865,10 @@ int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {
   // decoding sequences of up to 16384 tokens: 130 us with 1024 of them, 129 with 1536, 135 with 2048).
   const int64_t wgs = a.tiles * j.n_kv * j.n_seqs, all = j.n_tokens * j.n_heads;
   int64_t splits = cdiv(by_rows ? 512 : 1536, wgs);
-  const int64_t useful = cdiv(j.table_pages * j.page, 256);
+  // (decoding over up to 512 tokens goes undivided: the second launch costs a call 3 of 17 us, and
+  // two tiles of a wave less gain about as much on the device as joining takes)
+  const int64_t room = j.table_pages * j.page;
+  const int64_t useful = !by_rows && room <= 512 ? 1 : cdiv(room, 256);
   splits = splits < useful ? splits : useful;
   splits = splits < MAX_SPLITS ? splits : MAX_SPLITS;
   if (splits * all > split_rows(all)) splits = split_rows(all) / all;
