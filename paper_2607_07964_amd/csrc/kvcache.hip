@@ -781,8 +781,6 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs A, int n_seqs) {
     bool in = false;
     for (int b = lane; b < n_seqs; b += 64) in |= tok >= A.starts[b] && tok < A.starts[b + 1];
     if (!__any(in)) return;
-  } else if (tok >= n_seqs) {
-    return;
   }
   float mx = -INFINITY;
   for (int s = 0; s < A.splits; ++s) mx = fmaxf(mx, A.ml[2 * (s * rows + row)]);
@@ -863,7 +861,9 @@ int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {
   a.tiles = int(cdiv(rows, by_rows ? 64 * mq : 16 * mq));
   // Enough workgroups for sequences of different lengths to even out, of 256 tokens each at least (48
   // decoding sequences of up to 16384 tokens: 130 us with 1024 of them, 129 with 1536, 135 with 2048).
-  const int64_t wgs = a.tiles * j.n_kv * j.n_seqs, all = j.n_tokens * j.n_heads;
+  // (without starts, sequences from n_tokens on have no new token)
+  const int64_t n_seqs = j.starts || j.n_seqs < j.n_tokens ? j.n_seqs : j.n_tokens;
+  const int64_t wgs = a.tiles * j.n_kv * n_seqs, all = j.n_tokens * j.n_heads;
   int64_t splits = cdiv(by_rows ? 512 : 1536, wgs);
   // (decoding over up to 512 tokens goes undivided: the second launch costs a call 3 of 17 us, and
   // two tiles of a wave less gain about as much on the device as joining takes)
@@ -880,12 +880,12 @@ int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {
   a.part = cv.take<float>(cap * size_t(j.dim));
   a.ml = cv.take<float>(cap * 2);
   if (j.dim == 128)
-    return mq == 1   ? launch_attention<128, 1, false>(a, j.n_seqs, s)
-           : by_rows ? launch_attention<128, 2, true>(a, j.n_seqs, s)
-                     : launch_attention<128, 2, false>(a, j.n_seqs, s);
-  return mq == 1   ? launch_attention<64, 1, false>(a, j.n_seqs, s)
-         : by_rows ? launch_attention<64, 2, true>(a, j.n_seqs, s)
-                   : launch_attention<64, 2, false>(a, j.n_seqs, s);
+    return mq == 1   ? launch_attention<128, 1, false>(a, n_seqs, s)
+           : by_rows ? launch_attention<128, 2, true>(a, n_seqs, s)
+                     : launch_attention<128, 2, false>(a, n_seqs, s);
+  return mq == 1   ? launch_attention<64, 1, false>(a, n_seqs, s)
+         : by_rows ? launch_attention<64, 2, true>(a, n_seqs, s)
+                   : launch_attention<64, 2, false>(a, n_seqs, s);
 }
 
 }  // namespace kq

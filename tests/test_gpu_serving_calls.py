@@ -1,0 +1,57 @@
+"""Calls of the serving operators that their documentation allows and that lie off the beaten path:
+sequences without new tokens, no sequences at all, sizes at the limits, activations at both ends of
+fp32's range, sums that add up the roundings of a group. Through the C ABI against the float64 oracle,
+with the tolerances of the operators' own tests where nothing else is derived.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import oracle as O
+from gpu_util import DEV, note, rel_frob
+from paper_2607_07964_amd import kronq as K
+from test_gpu_cache import TOL as TOL_ATTENTION
+from test_gpu_cache import Cache, f64, randn
+from test_gpu_served import BF16, FP32, TOL, Layer, rows_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    K.load()
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+
+
+def attention_call(q, c, out, n_tokens, starts=None, most=1, flags=1, n_seqs=None):
+    """kronq_cache_attention as C has it, with a workspace of just the bytes it asks for."""
+    codes, params, table, lengths = c.dev()
+    heads, dim = q.shape[1:]
+    ws = torch.empty(K.kronq_workspace_bytes(K.OP_ATTENTION, heads, dim, n_tokens),
+                     dtype=torch.uint8, device=DEV)
+    ptr = lambda t: ctypes.c_void_p(None if t is None else t.data_ptr())  # noqa: E731
+    rc = K.load().kronq_cache_attention(
+        ptr(q), heads * dim, n_tokens, heads, c.kv, dim, ptr(codes), ptr(params), codes.shape[0],
+        c.page, ptr(table), table.shape[1], table.shape[1], ptr(lengths),
+        table.shape[0] if n_seqs is None else n_seqs, ptr(starts), most, dim ** -0.5, flags, ptr(out),
+        heads * dim, ptr(ws), ws.numel(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    torch.cuda.synchronize()
+    return rc
+
+
+@pytest.mark.parametrize("lengths,tokens", [([40, 90, 33, 70], 2), ([900, 1500, 700], 1),
+                                            ([1300, 40, 2000, 1, 999], 3)])
+def test_attention_of_fewer_tokens_than_sequences(lengths, tokens):
+    """Without starts, sequences from n_tokens on have no new token: neither rows of q behind the last
+    one are read nor rows of out written, undivided and with the tokens split over workgroups."""
+    c = Cache(lengths, 2, 128, 16, True, seed=31)
+    q = randn(len(lengths) + 2, 8, 128, seed=32)
+    q[tokens:] = float("nan")
+    out = torch.full((len(lengths) + 2, 8, 128), 3.0, dtype=BF16, device=DEV)
+    note(f"attention of {tokens} tokens over sequences {lengths}")
+    assert attention_call(q.to(DEV), c, out, tokens) == 0
+    ref = c.ref(f64(q[:tokens]), np.minimum(np.arange(len(lengths) + 1), tokens))
+    assert rel_frob(f64(out[:tokens]), ref) < TOL_ATTENTION
+    assert bool((out[tokens:] == 3).all())
