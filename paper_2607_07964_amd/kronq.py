@@ -144,6 +144,15 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(0)
 
 
+def _row_stride(t: torch.Tensor, least: int) -> int:
+    """Row stride of a 2-D tensor; that of a single row is free (``least`` stands for it), and so is
+    the column stride of a single column."""
+    rows, cols = t.shape
+    if rows == 0 or cols == 1 or t.stride(1) == 1:
+        return t.stride(0) if rows > 1 else least
+    raise ValueError("expected a row-major 2-D tensor (unit column stride)")
+
+
 def _dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.bfloat16:
         return KRONQ_BF16
@@ -505,10 +514,8 @@ def _served(func, packed, scales, zeros, bits, group, d_in, mul_in, mul_out, q28
         raise ValueError(f"y must be [{n} x {d_out}]")
     if residual is not None and (residual.shape != y.shape or residual.dtype != y.dtype):
         raise ValueError("residual must have y's shape and dtype")
-    # (a single row has any row stride)
-    ldx = _ld(x) if n > 1 else -(-d_in // 8) * 8
-    ldy = _ld(y) if n > 1 else d_out
-    ldr = 0 if residual is None else _ld(residual) if n > 1 else d_out
+    ldx, ldy = _row_stride(x, d_in), _row_stride(y, d_out)
+    ldr = 0 if residual is None else _row_stride(residual, d_out)
     with _guard(dev):
         if ws is None:
             need = lib.kronq_workspace_bytes(OP_LINEAR, d_out, d_in, n) if offsets is None else \
