@@ -443,7 +443,7 @@ int kronq_cache_append(const void* k, const void* v, int dtype, int64_t ldk, int
  *   lengths  device int32 [n_seqs]; cut to [0, table_pages * page].
  *   starts   device int32 [n_seqs + 1], ascending, cut to [0, n_tokens]; NULL: token b is the one
  *            new token of sequence b (n_tokens <= n_seqs). Tokens of no sequence keep what out
- *            holds, or get zeros with KRONQ_CACHE_FILL.
+ *            holds, or get zeros with KRONQ_CACHE_FILL (n_seqs = 0: all of them).
  *   max_new  host: at least one and about the largest number of new tokens of a sequence (it sizes
  *            the launch; a longer one is computed all the same, later).
  *   All of table, lengths and starts are read on the device, so that a captured call follows them.

@@ -220,6 +220,8 @@ struct AttentionJob {
   int64_t ldo;
 };
 size_t attention_ws_bytes(int64_t n_heads, int64_t dim, int64_t n_tokens);
+// zeros for the width values of every token (bf16)
+int cache_zeros_launch(void* out, int64_t ldo, int64_t n_tokens, int64_t width, hipStream_t s);
 int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s);
 // diagnostics: matrix statistics, Jacobi eigendecomposition, expected-loss factors
 size_t matrix_stats_ws_bytes(int64_t rows, int64_t cols);

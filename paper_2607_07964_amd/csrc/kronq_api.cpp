@@ -636,12 +636,13 @@ int kronq_cache_attention(const void* q, int64_t ldq, int64_t n_tokens, int64_t 
   KQ_REQUIRE(n_tokens >= 0 && n_tokens <= (int64_t(1) << 31) / (n_heads * 4),
              KRONQ_ERR_INVALID_ARG, "bad n_tokens");
   KQ_REQUIRE(n_seqs >= 0 && n_seqs <= 65535, KRONQ_ERR_UNSUPPORTED, "n_seqs must be at most 65535");
-  if (n_tokens == 0 || n_seqs == 0) return KRONQ_OK;
+  if (n_tokens == 0 || (n_seqs == 0 && !(flags & KRONQ_CACHE_FILL))) return KRONQ_OK;
+  KQ_REQUIRE(out && aligned(out, 2) && (n_tokens == 1 || ldo >= n_heads * dim),
+             KRONQ_ERR_INVALID_ARG, "out must be 2-byte aligned with ldo >= n_heads * dim");
+  if (n_seqs == 0) return kq::cache_zeros_launch(out, ldo, n_tokens, n_heads * dim, as_stream(stream));
   KQ_REQUIRE(q && aligned(q, 16) && ldq % 8 == 0 && (n_tokens == 1 || ldq >= n_heads * dim),
              KRONQ_ERR_INVALID_ARG,
              "q must be 16-byte aligned with ldq >= n_heads * dim, divisible by 8");
-  KQ_REQUIRE(out && aligned(out, 2) && (n_tokens == 1 || ldo >= n_heads * dim),
-             KRONQ_ERR_INVALID_ARG, "out must be 2-byte aligned with ldo >= n_heads * dim");
   KQ_REQUIRE(table && aligned(table, 4) && table_pages >= 1 && ldt >= table_pages &&
                  table_pages <= ((int64_t(1) << 30) / page),
              KRONQ_ERR_INVALID_ARG,

@@ -797,6 +797,13 @@ __global__ __launch_bounds__(256) void attention_join(AttnArgs A, int n_seqs) {
   store_row<DIM>(A.out + tok * A.ldo + (row % A.n_heads) * DIM, x, lane, A.rotate);
 }
 
+// zeros for tokens of no sequence where there is no sequence at all
+__global__ __launch_bounds__(256) void cache_zeros(uint16_t* out, int64_t ldo, int64_t n_tokens,
+                                                   int width) {
+  for (int64_t t = blockIdx.x; t < n_tokens; t += gridDim.x)
+    for (int e = threadIdx.x; e < width; e += 256) out[t * ldo + e] = 0;
+}
+
 // ---- plan and launches ---------------------------------------------------------------------------
 constexpr int64_t MAX_SPLITS = 32, SPLIT_ROWS = 131072;
 
@@ -840,6 +847,12 @@ size_t attention_ws_bytes(int64_t n_heads, int64_t dim, int64_t n_tokens) {
   if (n_heads <= 0 || dim <= 0 || n_tokens <= 0) return 0;
   const size_t rows = size_t(split_rows(n_heads * n_tokens));
   return align256(rows * size_t(dim) * 4) + align256(rows * 8);
+}
+
+int cache_zeros_launch(void* out, int64_t ldo, int64_t n_tokens, int64_t width, hipStream_t s) {
+  const int64_t groups = n_tokens < 65536 ? n_tokens : 65536;
+  return launch("cache_zeros", cache_zeros, dim3(static_cast<unsigned>(groups)), dim3(256), 0, s,
+                static_cast<uint16_t*>(out), ldo, n_tokens, int(width));
 }
 
 int cache_attention_launch(const AttentionJob& j, void* ws, hipStream_t s) {

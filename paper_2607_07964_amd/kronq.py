@@ -661,8 +661,8 @@ def kronq_cache_attention(q: torch.Tensor, codes: torch.Tensor, params: torch.Te
     _typed(starts, torch.int32, (seqs + 1,), "starts")
     if starts is None and n != seqs:
         raise ValueError("without starts there is one token per sequence")
-    if n == 0 or seqs == 0:
-        return out.zero_() if fill else out
+    if n == 0:
+        return out
     most = max_new if max_new is not None else 1 if starts is None else n
     ldt = table.stride(0) if seqs > 1 else table.shape[1]
     with _guard(dev):

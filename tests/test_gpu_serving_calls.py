@@ -55,3 +55,28 @@ def test_attention_of_fewer_tokens_than_sequences(lengths, tokens):
     ref = c.ref(f64(q[:tokens]), np.minimum(np.arange(len(lengths) + 1), tokens))
     assert rel_frob(f64(out[:tokens]), ref) < TOL_ATTENTION
     assert bool((out[tokens:] == 3).all())
+
+
+@pytest.mark.parametrize("tokens,heads,dim", [(1, 1, 64), (7, 4, 128), (70000, 2, 64)])
+def test_attention_without_sequences(tokens, heads, dim):
+    """Every token is one of no sequence: zeros where they are asked for, and nothing otherwise."""
+    codes, params = K.kronq_cache_empty(1, 1, dim, 16, DEV)
+    q = torch.randn(tokens, heads, dim, dtype=BF16, device=DEV)
+    rows = torch.full((tokens + 1, heads * dim + 3), 3.0, dtype=BF16, device=DEV)
+    nul, ptr = ctypes.c_void_p(0), lambda t: ctypes.c_void_p(t.data_ptr())
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    note(f"attention of {tokens} tokens without sequences")
+    for flags, want in ((1, 3.0), (3, 0.0)):
+        assert K.load().kronq_cache_attention(
+            ptr(q), heads * dim, tokens, heads, 1, dim, ptr(codes), ptr(params), 1, 16, nul, 0, 0, nul,
+            0, nul, 1, 0.1, flags, ptr(rows), heads * dim + 3, nul, 0, stream) == 0
+        torch.cuda.synchronize()
+        assert bool((rows[:tokens, :heads * dim] == want).all())
+        assert bool((rows[:, heads * dim:] == 3).all()) and bool((rows[tokens] == 3).all())
+    table, none = torch.zeros(0, 4, dtype=torch.int32, device=DEV), torch.zeros(0, dtype=torch.int32,
+                                                                              device=DEV)
+    starts = torch.zeros(1, dtype=torch.int32, device=DEV)
+    torch.full_like(q, float("nan"))  # (what the allocator hands out next is not zero)
+    out = K.kronq_cache_attention(q, codes, params, table, none, starts)
+    torch.cuda.synchronize()
+    assert out.shape == q.shape and not bool(out.any())
