@@ -328,8 +328,9 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
     if (A.fill) {  // tokens before the first sequence and behind the last one, dealt to all workgroups
       const int s0 = A.starts[0], s1 = A.starts[gridDim.y];
       const int head = s0 < 0 ? 0 : s0 > nt ? nt : s0, tail = s1 < head ? head : s1 > nt ? nt : s1;
-      const int all = int(gridDim.y * gridDim.z), width = A.group * DIM;
-      for (int64_t k = b + int(gridDim.y * blockIdx.z); k < head + nt - tail; k += all) {
+      const int64_t all = int64_t(gridDim.y) * gridDim.z;  // (may pass 2^31)
+      const int width = A.group * DIM;
+      for (int64_t k = b + int64_t(gridDim.y) * blockIdx.z; k < head + nt - tail; k += all) {
         uint16_t* const out = A.out + (k < head ? k : k - head + tail) * A.ldo + int64_t(h) * width;
         for (int e = tid; e < width; e += 256) out[e] = 0;
       }
