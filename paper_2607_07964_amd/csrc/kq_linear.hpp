@@ -77,16 +77,15 @@ int linear_in_launch(const LinearIn& a, hipStream_t s);
 
 // y = act(diag(mul_out) T_out y' + bias) + residual
 struct LinearOut {
-  // y' [row][ld]; dealt (workers > 0), with the parts that workers keep, [worker][32 nt][block]. Both
-  // fp16 to be multiplied by w_unit (with w_unit) or fp32.
-  const void* part;
+  // y' [row][ld] (with w_unit: to be multiplied by it); dealt (workers > 0), with the parts that workers
+  // keep, [worker][32 nt][block]
+  const float* part;
   int64_t ld;
   int workers, ng, nt, block, row_blocks, items;  // items without offsets
-  const void* kept;
+  const float* kept;
   const float* w_unit;
   const LinearTile* tiles;
   const int2* first;
-  float unit;             // of everything
   const float* row_unit;  // or null (1)
   int64_t n_rows, d_out;
   const float *mul, *q28;

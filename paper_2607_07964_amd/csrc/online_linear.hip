@@ -64,10 +64,9 @@ struct MmArgs {
   const Tile* tiles;  // null: one layer, unit tiles in order
   int64_t n_rows;
   int row_blocks;
-  void* part;         // [row][ld]
+  float* part;        // [row][ld]
   int64_t ld;
-  void* kept;         // [worker][32 NT][rows of W of an item]
-  float down;         // of fp16 results
+  float* kept;        // [worker][32 NT][rows of W of an item]
 };
 
 __device__ __forceinline__ f16x2_t h2(uint32_t v) { return __builtin_bit_cast(f16x2_t, v); }
@@ -381,8 +380,7 @@ __global__ __launch_bounds__(512, 2) void linear_few(MmArgs A) {
     // a worker that began inside an item keeps its part
     const int64_t ld = g0 > 0 ? BLOCK : A.ld, n = int64_t(rb) * BLOCK + mine;
     float* const part =
-        g0 > 0 ? static_cast<float*>(A.kept) + (int64_t(id) * NT - t.unit) * 32 * BLOCK - rb * BLOCK
-               : static_cast<float*>(A.part);
+        g0 > 0 ? A.kept + (int64_t(id) * NT - t.unit) * 32 * BLOCK - rb * BLOCK : A.part;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const int mu = (t.unit + i) * 32, m0 = mu + 4 * h;
@@ -408,8 +406,7 @@ __global__ __launch_bounds__(512, 2) void linear_few(MmArgs A) {
 // read one step of 16 columns ahead.
 //   SCALED, NT = 4, RT = 2 (many rows): the matrix instructions bound it. Two workgroups per CU (64 KB
 //     of LDS and 256 registers a lane each), so that one wave's spreading of codes runs beside the
-//     other's matrix instructions. Results leave as fp16 (linear_out multiplies by the units of the
-//     rows of W).
+//     other's matrix instructions.
 //   PLANES = 2, NT = 2, RT = 2: the same for fp32 results.
 // 8192 rows of 4096 x 4096 at 4 bits: 240 us, 1.15 PFLOP/s, where a large plain matrix product reaches
 // 1.22 to 1.32. A lane reads its row of W in batches; the fp32 scales and zeros (not SCALED) come
@@ -623,25 +620,22 @@ __global__ __launch_bounds__(256, 2) void linear_ring(MmArgs A) {
     wait_vm<0>();  // (loads past the end still write to LDS)
     __builtin_amdgcn_s_barrier();
     // a worker that began inside an item keeps its part
-    using Part = std::conditional_t<SCALED, _Float16, float>;
     const int64_t ld = g0 > 0 ? BLOCK : A.ld;
-    Part* const part =
-        g0 > 0 ? static_cast<Part*>(A.kept) + (int64_t(id) * NT - t.unit) * 32 * BLOCK - rb * BLOCK
-               : static_cast<Part*>(A.part);
+    float* const part =
+        g0 > 0 ? A.kept + (int64_t(id) * NT - t.unit) * 32 * BLOCK - rb * BLOCK : A.part;
 #pragma unroll
     for (int k = 0; k < RT; ++k) {
       const int64_t n = n0 + 32 * k + (lane & 31);
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
         const int mu = (t.unit + i) * 32, m0 = mu + 4 * (lane >> 5);
-        Part* p = part + int64_t(m0) * ld + n;
+        float* p = part + int64_t(m0) * ld + n;
         const bool whole = mu >= t.lo && mu + 32 <= t.hi;  // (uniform) every row of it is the tile's
         if (n < A.d_out) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int m = m0 + 8 * (r >> 2) + (r & 3);
-            const float v = SCALED ? acc[i][k][r] * A.down : acc[i][k][r];
-            if (whole || (m >= t.lo && m < t.hi)) *p = Part(v);
+            if (whole || (m >= t.lo && m < t.hi)) *p = acc[i][k][r];
             p += (r & 3) == 3 ? 5 * ld : ld;
           }
         }
@@ -658,7 +652,6 @@ constexpr int64_t GEMV_ROWS = 4, GEMV_INPUTS = 32768;
 struct Plan {
   int planes, nt, workers;
   bool scaled, few;
-  float down;
   int64_t tiles, row_blocks;
 };
 
@@ -677,16 +670,12 @@ Plan make_plan(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts, i
   p.tiles = n_experts == 1 ? cdiv(n_rows, 32 * p.nt) : most_tiles(n_rows, n_experts, p.nt);
   p.row_blocks = cdiv(d_out, BLOCK);
   p.workers = device_cus() / 8 * 8 * (p.few ? 1 : 2);
-  // fp16 results: below 2^8 (x') times 2.5 (|c - z| < 1280 of at most 2^-9) times d_in
-  p.down = 1.f;
-  while (p.scaled && 640.f * float(d_in) * p.down > 65000.f) p.down *= 0.5f;
   return p;
 }
 
 struct Ws {
   uint16_t* xf;
-  float *row_unit, *w_unit;
-  char *part, *kept;
+  float *row_unit, *w_unit, *part, *kept;
   uint32_t* table;
   Tile* tiles;
   int2* first;
@@ -699,9 +688,8 @@ Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, i
   Ws w;
   w.xf = cv.take<uint16_t>(size_t(p.planes) * size_t(cdiv(n_rows, 32) * 32) * size_t(d_in));
   w.row_unit = cv.take<float>(size_t(n_rows));
-  const size_t size = p.scaled ? 2 : 4;  // of a product
-  w.part = cv.take<char>(size_t(n_rows) * size_t(cdiv(d_out, 8) * 8) * size);
-  w.kept = cv.take<char>(size_t(p.workers) * size_t(32 * p.nt) * size_t(BLOCK) * size);
+  w.part = cv.take<float>(size_t(n_rows) * size_t(cdiv(d_out, 8) * 8));
+  w.kept = cv.take<float>(size_t(p.workers) * size_t(32 * p.nt) * size_t(BLOCK));
   const size_t w_rows = p.scaled ? size_t(n_experts) * size_t(d_out) : 0;
   w.w_unit = cv.take<float>(w_rows);
   w.table = cv.take<uint32_t>(w_rows * size_t(d_in / 128));
@@ -746,7 +734,7 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
     KQ_TRY(online_product_launch(j.packed, j.ldp, j.scales, j.zeros, j.ldsz, j.bits, j.group,
                                  j.d_out, j.d_in, j.mul_in, j.q28_in, j.flags, j.x, j.x_dtype,
                                  j.ldx, j.n_rows, ws, &yr, s));
-    o.part = yr, o.ld = j.d_out, o.unit = 1.f;
+    o.part = yr, o.ld = j.d_out;
     return linear_out_launch(o, s);
   }
   const Plan p = make_plan(j.d_out, j.d_in, j.n_rows, j.n_experts, j.y_dtype);
@@ -768,13 +756,13 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
   m.scales = j.scales, m.zeros = j.zeros, m.ldsz = j.ldsz, m.gpq = a.gpq;
   m.tiles = j.offsets ? w.tiles : nullptr, m.n_rows = j.n_rows;
   m.row_blocks = int(p.row_blocks);
-  m.part = w.part, m.ld = cdiv(j.d_out, 8) * 8, m.kept = w.kept, m.down = p.down;
+  m.part = w.part, m.ld = cdiv(j.d_out, 8) * 8, m.kept = w.kept;
   KQ_TRY(j.bits == 2   ? launch_mm<2>(m, p, s)
          : j.bits == 3 ? launch_mm<3>(m, p, s)
          : j.bits == 4 ? launch_mm<4>(m, p, s)
                        : launch_mm<8>(m, p, s));
   o.part = w.part, o.ld = m.ld, o.block = BLOCK;
-  o.row_unit = w.row_unit, o.unit = 1.f / p.down;
+  o.row_unit = w.row_unit;
   o.workers = p.workers, o.ng = a.ng, o.nt = p.nt, o.row_blocks = m.row_blocks, o.kept = w.kept;
   o.items = int(p.tiles * p.row_blocks), o.w_unit = p.scaled ? w.w_unit : nullptr;
   if (j.offsets) o.tiles = w.tiles, o.first = w.first;

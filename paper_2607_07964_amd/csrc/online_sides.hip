@@ -501,23 +501,16 @@ __device__ __forceinline__ float finish(float v, unsigned j, const float* mul, c
   return v;
 }
 
-__device__ __forceinline__ void load8(const _Float16* p, float* v) {
-  const f16x8_t w = *reinterpret_cast<const f16x8_t*>(p);
-#pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] = float(w[k]);
-}
-
-// Where a row's products lie. TP: their type.
-template <typename TP>
+// Where a row's products lie.
 struct Products {
   const LinearOut& A;
-  const TP* p;
+  const float* p;
   const float* w_unit;
   int64_t row;
   int item0, in_tile, full_items, per;  // dealt
 
   __device__ __forceinline__ Products(const LinearOut& a, int64_t r, int expert) : A(a), row(r) {
-    p = static_cast<const TP*>(A.part) + row * A.ld;
+    p = A.part + row * A.ld;
     w_unit = A.w_unit ? A.w_unit + int64_t(expert) * A.d_out : nullptr;
     if (A.workers == 0) return;
     const int u = int(row >> 5);
@@ -542,8 +535,8 @@ struct Products {
     from = r * A.ng / per + 1, to = ((r + 1) * A.ng - 1) / per + 1;
     to = to < A.workers ? to : A.workers;
   }
-  __device__ __forceinline__ const TP* kept(int worker, int j) const {
-    return static_cast<const TP*>(A.kept) + (int64_t(worker) * 32 * A.nt + in_tile) * A.block +
+  __device__ __forceinline__ const float* kept(int worker, int j) const {
+    return A.kept + (int64_t(worker) * 32 * A.nt + in_tile) * A.block +
            (j & (A.block - 1));  // (128 or 256)
   }
   // eight neighbours
@@ -576,7 +569,7 @@ struct Products {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       at[k] = j + k * step < d ? j + k * step : j;
-      v[k] = float(p[at[k]]);
+      v[k] = p[at[k]];
       from[k] = to[k] = 0;
       if (A.workers) parts(at[k], from[k], to[k]);
       most = max(most, to[k] - from[k]);
@@ -588,7 +581,7 @@ struct Products {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int w = from[k] + s + i;
-          u[k][i] = to[k] > from[k] ? float(*kept(w < to[k] ? w : to[k] - 1, at[k])) : 0.f;
+          u[k][i] = to[k] > from[k] ? *kept(w < to[k] ? w : to[k] - 1, at[k]) : 0.f;
         }
 #pragma unroll
       for (int k = 0; k < K; ++k)
@@ -642,7 +635,7 @@ __device__ __forceinline__ void finish_row(const LinearOut& A, const float* buf,
 }
 
 // C columns of a rotated row of whole octets
-template <typename TP, typename T, int C, bool FULL>
+template <typename T, int C, bool FULL>
 __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
   extern __shared__ __attribute__((aligned(16))) float buf[];  // the row
   constexpr int THR = threads(C), WAVES = THR / 64, N = (64 * C + THR - 1) / THR;
@@ -656,7 +649,7 @@ __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
   }
   __shared__ float factor[C % 28 == 0 ? 784 : 1];
   if constexpr (C % 28 == 0) stage28<THR>(factor, A.q28 + int64_t(expert) * 784, tid);
-  const Products<TP> products(A, row, expert);
+  const Products products(A, row, expert);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int at = 512 * (wave + WAVES * n), j = at + 8 * octet_of(lane);
@@ -673,7 +666,7 @@ __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
     }
   }
   __syncthreads();
-  const float unit = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
+  const float unit = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm;
   if constexpr (C % 28 == 0) {
     float q[14];
     load28<true>(q, factor, lane);
@@ -704,7 +697,7 @@ __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
 // one workgroup each takes 14.5; 32 of them 12.4 and 14.5; 64 of them 17.5 and 14.8, so that half of
 // the CUs is the limit.
 constexpr int PARTS = 4;
-template <typename TP, typename T, int B>
+template <typename T, int B>
 __global__ __launch_bounds__(1024) void linear_out_part(LinearOut A) {
   extern __shared__ __attribute__((aligned(16))) float buf[];  // the row, then the 7 segments
   __shared__ float factor[784];
@@ -719,7 +712,7 @@ __global__ __launch_bounds__(1024) void linear_out_part(LinearOut A) {
     if (expert < 0) return;
   }
   stage28<1024>(factor, A.q28 + int64_t(expert) * 784, tid);
-  const Products<TP> products(A, row, expert);
+  const Products products(A, row, expert);
 #pragma unroll 1
   for (int j = 8 * tid; j < d; j += 8192) {
     float v[8];
@@ -775,7 +768,7 @@ __global__ __launch_bounds__(1024) void linear_out_part(LinearOut A) {
     }
   }
   __syncthreads();
-  const float unit = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
+  const float unit = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm;
   const int half = cols / 2;  // (a power of two from 4 on)
   finish_row<T>(A, buf, row, expert, unit, 2 * (tid & (half - 1)), tid / half, 1024 / half,
                 first * m, 7 * m);
@@ -783,7 +776,7 @@ __global__ __launch_bounds__(1024) void linear_out_part(LinearOut A) {
 
 // Rows without a transform, and transforms whose columns are shorter than an octet (cols: 1, 2 or 4
 // elements in each of 28 or fewer columns: the dense product).
-template <typename TP, typename T>
+template <typename T>
 __global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
   __shared__ float small[128];
   const int tid = threadIdx.x, d = int(A.d_out);
@@ -793,16 +786,16 @@ __global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
     expert = expert_of(A.offsets, A.n_experts, row);
     if (expert < 0) return;
   }
-  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm * A.unit;
+  const float up = (A.row_unit ? A.row_unit[row] : 1.f) * A.turn.norm;
   const float* const mul = A.mul ? A.mul + int64_t(expert) * d : nullptr;
   const float* const bias = A.bias ? A.bias + int64_t(expert) * d : nullptr;
   const T* const res = A.residual ? static_cast<const T*>(A.residual) + row * A.ldr : nullptr;
   T* const y = static_cast<T*>(A.y) + row * A.ldy;
-  const Products<TP> products(A, row, expert);
+  const Products products(A, row, expert);
   constexpr int K = 4;
   for (int j = tid; j < d; j += 256 * K) {
     float v[K];
-    products.template sum_each<K>(j, 256, d, v);
+    products.sum_each<K>(j, 256, d, v);
     if (A.turn.rotate) {
       small[j] = v[0];  // (d <= 28 * 4)
       break;
@@ -867,7 +860,7 @@ int in_typed(const LinearIn& a, hipStream_t s) {
 #undef KQ_IN
 }
 
-template <typename TP, typename T>
+template <typename T>
 int out_typed(LinearOut a, hipStream_t s) {
   // two neighbours at once where every row of each operand begins on two
   const size_t pair = 2 * sizeof(T);
@@ -875,15 +868,15 @@ int out_typed(LinearOut a, hipStream_t s) {
             (!a.residual || (aligned(a.residual, pair) && a.ldr % 2 == 0));
   const dim3 grid(static_cast<unsigned>(a.n_rows));
   if (!a.turn.rotate || a.turn.cols < 8)
-    return launch("linear_out", linear_out_any<TP, T>, grid, dim3(256), 0, s, a);
+    return launch("linear_out", linear_out_any<T>, grid, dim3(256), 0, s, a);
 #define KQ_OUT(C_, F_) \
-  launch("linear_out", linear_out<TP, T, C_, F_>, grid, dim3(threads(C_)), size_t(a.d_out) * 4, s, a)
+  launch("linear_out", linear_out<T, C_, F_>, grid, dim3(threads(C_)), size_t(a.d_out) * 4, s, a)
   if (a.turn.has28 && a.n_rows * PARTS <= device_cus() / 2) {
     const dim3 parts(static_cast<unsigned>(a.n_rows * PARTS));
     return a.turn.m == 1024
-               ? launch("linear_out", linear_out_part<TP, T, 2>, parts, dim3(1024),
+               ? launch("linear_out", linear_out_part<T, 2>, parts, dim3(1024),
                         size_t(a.d_out) * 4, s, a)
-               : launch("linear_out", linear_out_part<TP, T, 1>, parts, dim3(1024),
+               : launch("linear_out", linear_out_part<T, 1>, parts, dim3(1024),
                         size_t(a.d_out) * 4, s, a);
   }
   const bool full = a.turn.cols == 512;
@@ -926,8 +919,7 @@ int linear_in_launch(const LinearIn& a, hipStream_t s) {
   return a.x_dtype == KRONQ_BF16 ? in_typed<uint16_t>(a, s) : in_typed<float>(a, s);
 }
 int linear_out_launch(const LinearOut& a, hipStream_t s) {
-  if (a.w_unit) return out_typed<_Float16, uint16_t>(a, s);  // (bf16 outputs alone take fp16 products)
-  return a.y_dtype == KRONQ_BF16 ? out_typed<float, uint16_t>(a, s) : out_typed<float, float>(a, s);
+  return a.y_dtype == KRONQ_BF16 ? out_typed<uint16_t>(a, s) : out_typed<float>(a, s);
 }
 
 }  // namespace kq

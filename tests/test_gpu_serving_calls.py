@@ -80,3 +80,27 @@ def test_attention_without_sequences(tokens, heads, dim):
     out = K.kronq_cache_attention(q, codes, params, table, none, starts)
     torch.cuda.synchronize()
     assert out.shape == q.shape and not bool(out.any())
+
+
+def whole_numbers(d_out, d_in, bits, experts=1):
+    """A layer without transforms whose scales are one power of two: with small whole activations every
+    product and every sum is a whole number times it, so that only the result is rounded."""
+    la = Layer(d_out, d_in, bits, 128, 0, experts=experts, bias=False)
+    la.scales[:], la.mul_in[:], la.mul_out[:] = 2.0 ** -7, 1.0, 1.0
+    la.device()
+    return la
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4, 8])
+@pytest.mark.parametrize("rows,d_out,d_in", [(300, 200, 4096), (700, 513, 2176), (257, 64, 128)])
+def test_whole_numbers_are_rounded_once(bits, rows, d_out, d_in):
+    """Many rows, few items, columns split over many workers: the sums are exact in fp32 (below 2^24
+    of their unit), so that the result is the bf16 value next to them, bit for bit."""
+    la = whole_numbers(d_out, d_in, bits)
+    x = torch.randint(-8, 9, (rows, d_in), generator=torch.Generator().manual_seed(rows)).to(BF16)
+    note(f"whole numbers bits={bits} rows={rows} {d_out}x{d_in}")
+    y = K.kronq_online_linear(*la.args, None, None, None, None, x.to(DEV), flags=0)
+    torch.cuda.synchronize()
+    ref = torch.from_numpy(la.ref(f64(x)))
+    assert float(ref.abs().max()) * 2 ** 7 < 2 ** 24
+    assert torch.equal(y.cpu(), ref.to(FP32).to(BF16))
