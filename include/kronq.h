@@ -360,9 +360,9 @@ int kronq_online_matvec(const uint32_t* packed, int64_t ldp, const float* scales
  *   residual device [n_rows x ldr], y's type, or NULL; may be y itself.
  *   y        device [n_rows x ldy], y_dtype KRONQ_BF16 or KRONQ_FP32, rows aligned to the element;
  *            must not overlap x.
- * Precision: a KRONQ_BF16 result takes the transformed activations and, with many rows, the
- * dequantised weights rounded to fp16 (each row scaled by a power of two; a quantisation group
- * whose scale is below 2^-8 of its row's largest keeps fewer than 11 bits), summed in fp32. A
+ * Precision: a KRONQ_BF16 result takes the transformed activations and, with many rows, the scales
+ * and the dequantised weights rounded to fp16 (each row scaled by a power of two; a quantisation group
+ * whose scale is below 2^-14 of its row's largest keeps fewer than 11 bits), summed in fp32. A
  * KRONQ_FP32 result takes activations of 22 bits (none coarser than 2^-32 of the row's largest)
  * and exact weights. Up to 4 rows with n_rows * d_in <= 32768 take kronq_online_matvec's.
  * n_rows = 0 does nothing. d_in <= 32768 (a multiple of 128), d_out <= 32768, n_rows <= 2^24,

@@ -58,7 +58,7 @@ struct LinearIn {
   uint16_t* xf;     // plane after plane
   int64_t plane;    // elements of a plane
   float* row_unit;  // [n_rows] what the rows were divided by
-  // the weights' table (or null): per group and row a dword {s 2^24 / unit, -z s / unit} in fp16;
+  // the weights' table (or null): per group and row a dword {s / unit, -(1024 + z)} in fp16;
   // per row its unit
   uint32_t* table;
   float* w_unit;

@@ -12,12 +12,12 @@
 //      to fp16 in registers.
 //   3. linear_out: the transform of y', and the epilogue.
 // Weights enter the matrix products in one of two forms (SCALED below): as fp16 s (c - z), each row
-// of W divided by a power of two, from a table of fp16 scales and offsets that linear_in prepares
-// (many rows of x: a multiply-add a pair of codes is all there is to do); or as the exact integers
-// c - z, each group's sum taking its fp32 scale (few rows, where the table would cost more than the
-// sums, and fp32 outputs).
-// Precision. For bf16 outputs x' (and s (c - z)) is rounded to fp16, 2^-11 against the output's own
-// 2^-8, and summed in fp32. For fp32 outputs x' is held in two fp16 planes (value and rest: 22 bits,
+// of W divided by a power of two, from a table of fp16 scales and zeros that linear_in prepares
+// (many rows of x: an AND, an addition and a multiplication a pair of codes are all there is to do); or
+// as the exact integers c - z, each group's sum taking its fp32 scale (few rows, where the table would
+// cost more than the sums, and fp32 outputs).
+// Precision. For bf16 outputs x' (and with the table s, and its product with the exact c - z) is rounded
+// to fp16, 2^-11 against the output's own 2^-8, and summed in fp32. For fp32 outputs x' is held in two fp16 planes (value and rest: 22 bits,
 // and never coarser than 2^-32 of the row's largest value) and the weights are exact.
 #include <cmath>
 #include <type_traits>
@@ -89,32 +89,40 @@ __device__ __forceinline__ uint32_t field3(const uint32_t* w, int jj) {
   }
 }
 
-// The eight codes of step jj of a chunk as fp16 weights s (c - z): code bits left where they stand
-// (as long as they stay below bit 10) are the subnormal c 2^(shift - 24), and one fused multiply-add
-// a pair makes the weight, rounded once. sz: fp16 {s 2^24, -z s}.
+// The eight codes of step jj of a chunk as fp16 weights s (c - z). A field of code bits at `shift` under
+// 0x6400 is 1024 + c 2^shift, and adding -(1024 + z 2^shift) leaves (c - z) 2^shift exactly (|z| < 1024:
+// a multiple of 2^shift below 2^11 of them), so that the product alone is rounded. (One fused
+// multiply-add with -z s as fp16 saves an instruction a pair, and its rounding moves all weights of
+// a group by the same amount: 8 bits and activations of mean 3, 6e-3 of the result.)
+// sz: fp16 {s / unit, -(1024 + z)}.
 template <int BITS>
 __device__ __forceinline__ u32x4_t spread(const uint32_t* w, int jj, uint32_t sz) {
-  const _Float16 s = h2(sz)[0], z = h2(sz)[1];
-  auto fma2 = [&](uint32_t v, int shift) {
-    const _Float16 t = s * _Float16(1.f / float(1 << shift));
-    return u2(__builtin_elementwise_fma(h2(v), f16x2_t{t, t}, f16x2_t{z, z}));
+  const _Float16 s = h2(sz)[0], nz = h2(sz)[1];
+  uint32_t base = 0x64006400u;
+  asm("" : "+v"(base));  // (in a register, mask and base make one instruction)
+  auto weights = [&](uint32_t v, int shift) {
+    const float up = float(1 << shift);
+    const _Float16 t = s * _Float16(1.f / up);
+    const _Float16 n =
+        shift ? __builtin_elementwise_fma(nz, _Float16(up), _Float16(1024.f * (up - 1.f))) : nz;
+    return u2((h2(v | base) + f16x2_t{n, n}) * f16x2_t{t, t});
   };
   if constexpr (BITS == 2) {
-    const uint32_t v = w[jj >> 1] >> (8 * (jj & 1));
-    return u32x4_t{fma2(v & 0x00030003u, 0), fma2(v & 0x000C000Cu, 2), fma2(v & 0x00300030u, 4),
-                   fma2(v & 0x00C000C0u, 6)};
+    const uint32_t v = w[jj >> 1] >> (8 * (jj & 1)), v4 = v >> 4;
+    return u32x4_t{weights(v & 0x00030003u, 0), weights(v & 0x000C000Cu, 2),
+                   weights(v4 & 0x00030003u, 0), weights(v4 & 0x000C000Cu, 2)};
   } else if constexpr (BITS == 3) {
-    const uint32_t v = halves3(field3(w, jj));
-    return u32x4_t{fma2(v & 0x00070007u, 0), fma2(v & 0x00380038u, 3), fma2(v & 0x01C001C0u, 6),
-                   fma2((v >> 9) & 0x00070007u, 0)};
+    const uint32_t v = halves3(field3(w, jj)), v6 = v >> 6;
+    return u32x4_t{weights(v & 0x00070007u, 0), weights(v & 0x00380038u, 3),
+                   weights(v6 & 0x00070007u, 0), weights(v6 & 0x00380038u, 3)};
   } else if constexpr (BITS == 4) {
     const uint32_t v = w[jj], v8 = v >> 8;
-    return u32x4_t{fma2(v & 0x000F000Fu, 0), fma2(v & 0x00F000F0u, 4), fma2(v8 & 0x000F000Fu, 0),
-                   fma2(v8 & 0x00F000F0u, 4)};
+    return u32x4_t{weights(v & 0x000F000Fu, 0), weights(v & 0x00F000F0u, 4),
+                   weights(v8 & 0x000F000Fu, 0), weights(v8 & 0x00F000F0u, 4)};
   } else {
     const uint32_t a = w[2 * jj], b = w[2 * jj + 1];
-    return u32x4_t{fma2(a & 0x00FF00FFu, 0), fma2((a >> 8) & 0x00FF00FFu, 0),
-                   fma2(b & 0x00FF00FFu, 0), fma2((b >> 8) & 0x00FF00FFu, 0)};
+    return u32x4_t{weights(a & 0x00FF00FFu, 0), weights((a >> 8) & 0x00FF00FFu, 0),
+                   weights(b & 0x00FF00FFu, 0), weights((b >> 8) & 0x00FF00FFu, 0)};
   }
 }
 

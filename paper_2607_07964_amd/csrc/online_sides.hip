@@ -98,16 +98,16 @@ __device__ void fill_table(const LinearIn& A, int64_t block, int* sh) {
   for (int g = t; g < nq; g += PER) mx = fmaxf(mx, fabsf(s[g]));
 #pragma unroll
   for (int o = 1; o < PER; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-  // s 2^24 / unit in [2^14, 2^15): unit = 2^(e + 10) for a largest scale in [2^e, 2^(e + 1))
+  // the largest s / unit in [2^4, 2^5): |s (c - z)| / unit < 2^5 * 1280, inside fp16, and groups down to
+  // 2^-14 of the row's largest scale stay normal beside the shifted codes (times 2^-4)
   const int e = int(__float_as_uint(mx) >> 23) - 127;
-  const int ue = mx > 0.f && e < 128 ? clampi(e + 10, -100, 120) : 0;
+  const int ue = mx > 0.f && e < 128 ? clampi(e - 4, -122, 123) : 0;
   const float up = pow2f(-ue);
   if (t == 0) A.w_unit[row] = pow2f(ue);
   for (int g0 = 0; g0 < A.ng; g0 += 32) {
     for (int g = g0 + t; g < g0 + 32 && g < A.ng; g += PER) {
       const int q = g / A.gpq;
-      const float sn = s[q] * up;
-      const f16x2_t o = {_Float16(sn * 16777216.f), _Float16(-z[q] * sn)};
+      const f16x2_t o = {_Float16(s[q] * up), _Float16(-1024.f - z[q])};
       sh[(g - g0) * (TABLE_ROWS + 1) + r] = __builtin_bit_cast(int, o);
     }
     __syncthreads();

@@ -104,3 +104,99 @@ def test_whole_numbers_are_rounded_once(bits, rows, d_out, d_in):
     ref = torch.from_numpy(la.ref(f64(x)))
     assert float(ref.abs().max()) * 2 ** 7 < 2 ** 24
     assert torch.equal(y.cpu(), ref.to(FP32).to(BF16))
+
+
+@pytest.mark.parametrize("bits", [3, 4, 8])
+@pytest.mark.parametrize("experts,rows", [(1, 300), (3, 400)])
+def test_weights_of_both_signs_cancel(bits, experts, rows):
+    """As many weights s 2^k as -s 2^k in every group, and activations that are all alike: the
+    definition gives zero, and so does any rounding of s and of the weights that is the same for both
+    signs, but for the sums' own. An offset that the weights of a group share would add up."""
+    la = Layer(160, 1024, bits, 128, 0, experts=experts, bias=False)
+    r = np.random.default_rng(bits)
+    k = np.exp2(r.integers(0, bits - 2, (experts, 160, 8, 64))).astype(np.int64)
+    whole = r.permuted(np.concatenate((k, -k), -1), axis=-1)
+    zeros = r.integers(2 ** (bits - 2), 3 * 2 ** (bits - 2) + 1, (experts, 160, 8))  # |whole| from both ends
+    assert np.abs(whole).max() <= 2 ** (bits - 2)
+    la.zeros, la.codes = zeros.astype(np.float32), (whole + zeros[..., None]).astype(np.uint8)
+    whole, la.codes = (t.reshape(experts, 160, 1024) for t in (whole, la.codes))
+    assert np.array_equal(la.codes - np.repeat(zeros, 128, -1), whole)
+    la.mul_in[:], la.mul_out[:] = 1.0, 1.0
+    la.device()
+    x = torch.full((rows, 1024), 2.625, dtype=BF16, device=DEV)
+    note(f"weights that cancel bits={bits} experts={experts}")
+    if experts == 1:
+        y = K.kronq_online_linear(*la.args, None, None, None, None, x, flags=0)
+    else:
+        offsets = torch.tensor([0, 100, 290, 400], dtype=torch.int32, device=DEV)
+        y = K.kronq_online_grouped(*la.args, None, None, None, None, x, offsets, flags=0)
+    torch.cuda.synchronize()
+    # A product s 2^k 21 2^j has 11 + 5 bits beside 2^k, a partial sum of a group up to 64 of the largest
+    # more: 11 + 5 + 6 + 5 bits with 8-bit codes (k <= 5), beyond fp32's 24. Each of 1024 additions is
+    # then off by at most 2^-23 of a partial sum (cut off or rounded), which is at most half of the sum
+    # of all |w x| of a group (as much of it is positive as negative). The shared offset of s and z s
+    # rounded apart is up to 2^-11 * 128 s for each of 128 weights of 8 groups, some hundred times this.
+    half_sum = (np.abs(whole).reshape(experts, 160, 8, 128).sum(-1) / 2 * la.scales * 2.625).max(-1)
+    bound = 1024 * 2.0 ** -23 * half_sum.max(0)
+    assert np.all(np.abs(f64(y)) <= bound)
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4, 8])
+@pytest.mark.parametrize("experts,rows", [(1, 300), (3, 400)])
+@pytest.mark.parametrize("mean", [1.0, 3.0])
+def test_activations_of_nonzero_mean(bits, experts, rows, mean):
+    """Many rows (the table of fp16 scales). A scale is off by 2^-11 for all of its group, a weight and
+    an activation by 2^-11 each, independently of the next group's or column's: 3 * 2^-11 beside the
+    result's 2^-8."""
+    la = Layer(224, 2048, bits, 128, 0, experts=experts, bias=False)
+    r, top = np.random.default_rng(bits), 2 ** bits - 1  # codes of min-max grids of normal values
+    la.codes = np.clip(np.rint(r.normal(top / 2, top / 5.4, la.codes.shape)), 0, top).astype(np.uint8)
+    la.zeros = np.clip(np.rint(r.normal(top / 2, 0.3, la.zeros.shape)), 0, top).astype(np.float32)
+    la.mul_in[:] = 1.0
+    la.device()
+    x = (rows_of(rows, 2048, FP32) + mean).to(BF16)
+    note(f"activations of mean {mean} bits={bits} experts={experts}")
+    if experts == 1:
+        y, cuts = K.kronq_online_linear(*la.one(), x.to(DEV), flags=0), [0, rows]
+    else:
+        cuts = [0, 100, 290, 400]
+        y = K.kronq_online_grouped(*la.args, *la.factors, x.to(DEV),
+                                   torch.tensor(cuts, dtype=torch.int32, device=DEV), flags=0)
+    torch.cuda.synchronize()
+    ref = np.concatenate([la.ref(f64(x)[a:b], e=e) for e, (a, b) in enumerate(zip(cuts, cuts[1:]))])
+    assert rel_frob(f64(y), ref) < 2.0 ** -8 + 3 * 2.0 ** -11
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4, 8])
+def test_many_rows_with_zeros_outside_the_codes(bits):
+    la = Layer(96, 256, bits, 128, 0)
+    la.zeros = np.random.default_rng(bits).integers(-1024, 1024, la.zeros.shape).astype(np.float32)
+    la.zeros[0, :4, 0] = -1024, 1023, -1023, 1022
+    la.device()
+    x = rows_of(300, 256, BF16) + 0.5
+    note(f"many rows, zeros far outside bits={bits}")
+    y = K.kronq_online_linear(*la.one(), x.to(DEV), bias=la.bias_d[0], flags=0)
+    torch.cuda.synchronize()
+    assert rel_frob(f64(y), la.ref(f64(x))) < TOL[BF16]
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4, 8])
+def test_many_rows_with_scales_of_many_sizes(bits):
+    """Groups of a row whose scales lie up to 2^14 apart, rows of W of different sizes: activations in
+    one group of columns at a time, so that each group's weights are seen by themselves."""
+    la = Layer(192, 1024, bits, 128, 0, bias=False)
+    size = np.exp2([0.0, -3, -6, -8, -10, -12, -13, -13])
+    la.scales = (np.random.default_rng(1).uniform(1, 2, la.scales.shape) * size
+                 * np.exp2(np.arange(192) % 40 - 20.0)[:, None]).astype(np.float32)
+    la.mul_in[:], la.mul_out[:] = 1.0, 1.0
+    la.device()
+    x = torch.zeros(8 * 40, 1024)
+    for g in range(8):
+        x[40 * g:40 * g + 40, 128 * g:128 * g + 128] = rows_of(40, 128, FP32, seed=g) + 0.5
+    x = x.to(BF16)
+    note(f"many rows, scales of many sizes bits={bits}")
+    y = K.kronq_online_linear(*la.one(), x.to(DEV), flags=0)
+    torch.cuda.synchronize()
+    ref = la.ref(f64(x))
+    unit = np.repeat(la.scales[0], 40, axis=1).T  # [row of x, row of W]: the scale of its group
+    assert rel_frob(f64(y) / unit, ref / unit) < TOL[BF16]
