@@ -364,7 +364,9 @@ int kronq_online_matvec(const uint32_t* packed, int64_t ldp, const float* scales
  * and the dequantised weights rounded to fp16 (each row scaled by a power of two; a quantisation group
  * whose scale is below 2^-14 of its row's largest keeps fewer than 11 bits), summed in fp32. A
  * KRONQ_FP32 result takes activations of 22 bits (none coarser than 2^-32 of the row's largest)
- * and exact weights. Up to 4 rows with n_rows * d_in <= 32768 take kronq_online_matvec's.
+ * and exact weights. Rows whose largest transformed activation is below 2^-112 have fewer bits, and
+ * a transform's sums, before its norm, are those of fp32. Up to 4 rows with n_rows * d_in <= 32768
+ * take kronq_online_matvec's.
  * n_rows = 0 does nothing. d_in <= 32768 (a multiple of 128), d_out <= 32768, n_rows <= 2^24,
  * ldp and ldsz <= 2^20. Workspace: KRONQ_OP_LINEAR; calls that may run at once need one each. */
 int kronq_online_linear(const uint32_t* packed, int64_t ldp, const float* scales,

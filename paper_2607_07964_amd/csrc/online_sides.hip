@@ -414,7 +414,8 @@ __global__ __launch_bounds__(in_threads(C)) void linear_in(LinearIn A, int table
   for (int i = 1; i < WAVES; ++i) mx = fmaxf(mx, red[i]);
   mx *= A.turn.norm;
   const int e = int(__float_as_uint(mx) >> 23) - 127;
-  const int ue = mx > 0.f && e < 128 ? clampi(e - 7, -100, 100) : 0;
+  // (up to fp32's largest; below 2^-112 the row is left smaller, and its unit a normal number)
+  const int ue = mx > 0.f && e < 128 ? clampi(e - 7, -119, 120) : 0;
   float up = pow2f(-ue) * A.turn.norm;
   if (tid == 0) A.row_unit[row] = pow2f(ue);
   const int octet = octet_of(lane);

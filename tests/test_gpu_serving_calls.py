@@ -200,3 +200,37 @@ def test_many_rows_with_scales_of_many_sizes(bits):
     ref = la.ref(f64(x))
     unit = np.repeat(la.scales[0], 40, axis=1).T  # [row of x, row of W]: the scale of its group
     assert rel_frob(f64(y) / unit, ref / unit) < TOL[BF16]
+
+
+@pytest.mark.parametrize("exponent", [-112, -104, -93, 105, 116, 122])
+@pytest.mark.parametrize("rows", [20, 70, 300])
+@pytest.mark.parametrize("flags", [0, K.ROT_IN | K.ROT_OUT])
+def test_activations_at_both_ends_of_the_range(exponent, rows, flags):
+    """Rows whose largest value lies next to the ends of fp32 (those of 2^4 more and less beside them),
+    and weights that bring the results back: as exact as others."""
+    la = Layer(256, 512, 4, 128, flags, bias=False)
+    la.scales = np.ldexp(la.scales, -exponent * 4 // 5).astype(np.float32)
+    la.mul_in, la.mul_out = np.sign(la.mul_in), np.sign(la.mul_out)
+    la.device()
+    x = rows_of(rows, 512, FP32)
+    x /= x.abs().amax(1, keepdim=True)
+    x *= torch.exp2(exponent + (torch.arange(rows) % 5).float()[:, None])
+    note(f"activations of 2^{exponent} rows={rows} flags={flags}")
+    y = K.kronq_online_linear(*la.one(), x.to(DEV), flags=flags, out_dtype=BF16)
+    y32 = K.kronq_online_linear(*la.one(), x.to(DEV), flags=flags)
+    torch.cuda.synchronize()
+    unit = f64(x.abs().amax(1, keepdim=True))
+    got, got32, ref = f64(y) / unit, f64(y32) / unit, la.ref(f64(x)) / unit
+    if flags:
+        # The sums of the transform come before its norm, and with the largest exponent some pass fp32's
+        # largest number (22 * 2^126 = 2^130.5): those rows are not finite, as in any fp32 sum. A row
+        # goes either way if only a sum on the way may.
+        xm = f64(x) * la.mul_in[0]
+        over = np.abs(xm @ O.hadamard(512)).max(1) >= 2.0 ** 128
+        fine = np.isfinite(got).all(1)
+        assert over.any() == (exponent == 122) and np.array_equal(fine, np.isfinite(got32).all(1))
+        assert not np.isfinite(got[over]).any() and not np.isfinite(got32[over]).any()
+        assert fine.any() and fine[np.abs(xm).sum(1) < 2.0 ** 128].all()
+        got, got32, ref = got[fine], got32[fine], ref[fine]
+    assert rel_frob(got, ref) < TOL[BF16]
+    assert rel_frob(got32, ref) < TOL[FP32]
