@@ -584,10 +584,11 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
               if (s[i][f][r] == -INFINITY) w0 = 0.f;
               if (s[i][f][r + 1] == -INFINITY) w1 = 0.f;
             }
-            zs[i] = fmaf(w0, z0, zs[i]);
-            zs[i] = fmaf(w1, z1, zs[i]);
-            pf[i][2 * f + (r >> 1)] =
-                __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{w0, w1}, f16x2_t));
+            // (the zeros take the rounded weights too: their errors go with c - z then, not with c)
+            const f16x2_t w = __builtin_convertvector(f32x2_t{w0, w1}, f16x2_t);
+            zs[i] = fmaf(float(w[0]), z0, zs[i]);
+            zs[i] = fmaf(float(w[1]), z1, zs[i]);
+            pf[i][2 * f + (r >> 1)] = __builtin_bit_cast(uint32_t, w);
           }
         }
       __builtin_amdgcn_sched_barrier(0);

@@ -234,3 +234,41 @@ def test_activations_at_both_ends_of_the_range(exponent, rows, flags):
         got, got32, ref = got[fine], got32[fine], ref[fine]
     assert rel_frob(got, ref) < TOL[BF16]
     assert rel_frob(got32, ref) < TOL[FP32]
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("tokens,new", [(2, 1), (3, 1), (5, 5), (8, 1), (8, 8), (33, 33)])
+def test_values_whose_codes_are_their_zeros(dim, tokens, new):
+    """Channels that hold zero for every token stay zero but for the rounding of fp32 sums, whatever the
+    weights are rounded to: the codes' sum and the zeros' sum, each of up to 40 terms of at most 15 of the
+    largest scale and weights that add up to one, off by 40 * 2^-24 of that at most, and as much again for
+    the changes of reference."""
+    r = np.random.default_rng(tokens + dim)
+    heads, page = 24, 64
+    codes, params = K.kronq_cache_empty(1, 1, dim, page, DEV)
+    value = r.integers(0, 16, (page, dim))
+    scale = O.round_up_bf16(np.exp(0.3 * r.standard_normal((2, page))))
+    zero = r.integers(0, 16, (2, page))
+    value[:, 5:20] = zero[1][:, None]
+    words = np.stack([O.cache_words(r.integers(0, 16, (page, dim)), 0), O.cache_words(value, 1)])
+    codes.copy_(torch.from_numpy(words.view(np.int32))[None, None])
+    held = scale.astype(np.float32).view(np.uint32) | zero.astype(np.uint32)
+    params.copy_(torch.from_numpy(held.view(np.int32))[None, None])
+    q = randn(new, heads, dim, seed=tokens) * 0.2
+    starts = torch.tensor([0, new], dtype=torch.int32, device=DEV)
+    note(f"values of zero dim={dim} tokens={tokens} new={new}")
+    o = K.kronq_cache_attention(q.to(DEV), codes, params, torch.zeros(1, 1, dtype=torch.int32, device=DEV),
+                                torch.tensor([tokens], dtype=torch.int32, device=DEV), starts, new,
+                                rotate=False)
+    torch.cuda.synchronize()
+    k = scale[0][:, None] * (codes_of(words[0], dim) - zero[0][:, None])
+    v = scale[1][:, None] * (value - zero[1][:, None])
+    ref = O.causal_attention(f64(q), k[:tokens, None], v[:tokens, None], dim ** -0.5)
+    assert rel_frob(f64(o), ref) < TOL_ATTENTION
+    assert np.abs(f64(o)[:, :, 5:20]).max() <= 4 * 40 * 2.0 ** -24 * 15 * scale[1].max()
+
+
+def codes_of(words, dim):
+    """The codes of packed key words."""
+    w = words.reshape(-1, dim // 8, 1) >> (4 * np.arange(8, dtype=np.uint32))
+    return (w & 15).reshape(-1, dim).astype(np.int64)
