@@ -450,7 +450,7 @@ int kronq_cache_append(const void* k, const void* v, int dtype, int64_t ldk, int
  *            the launch; a longer one is computed all the same, later).
  *   All of table, lengths and starts are read on the device, so that a captured call follows them.
  * Precision: rotated queries and the weights p (times the value's scale) in fp16, the latter not
- * coarser than 2^-25 of the largest value scale; sums in fp32.
+ * coarser than 2^-25 of the largest value scale that a query sees; sums in fp32.
  *   flags   KRONQ_CACHE_ROTATE (as rotate of kronq_cache_append), KRONQ_CACHE_FILL.
  *   n_heads a multiple of n_kv; dim, page as in kronq_cache_append; n_seqs <= 65535,
  *   n_kv <= 65535. n_tokens = 0 does nothing. Workspace: KRONQ_OP_ATTENTION. */

@@ -235,11 +235,11 @@ __global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
 //   weights  p = 2^(S - m) with m a reference that follows the running maximum only when that
 //            leaves it by more than 2^7, so that most tiles rescale nothing and compare without
 //            crossing lanes. The weight that meets the value codes is p s_t / sigma as fp16, sigma
-//            following the largest value scale the same way.
+//            following the row's largest value scale the same way.
 //   outputs  O[row][channel] += (p s) c: the lane that held S for a row and four tokens of either
 //            half holds its weights for the same tokens as the A operand (the order of tokens in a
 //            sum is free), so nothing crosses lanes; sum (p s) z beside it.
-// fp16 for q (2^-11), for the weights (2^-11, and never coarser than 2^-25 of the largest value
+// fp16 for q (2^-11), for the weights (2^-11, and never coarser than 2^-25 of the row's largest value
 // scale); everything summed in fp32; outputs bf16.
 struct AttnArgs {
   const uint16_t* q;
@@ -415,9 +415,15 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
     f32x4_t acc[MQ][ND] = {};
     // the reference m of a row (NONE: it has seen no token), what is subtracted from its scores, and
     // how far above it they may be
-    float m[MQ], ref[MQ], above[MQ], l[MQ], zs[MQ], sigma = 0.f, sinv = 0.f;
+    float m[MQ], ref[MQ], above[MQ], l[MQ], zs[MQ];
+    // what the row's weights are divided by: within 2^7 of the largest value scale that it has seen (not
+    // that the wave has: a later token's would take the weights of the rows before it)
+    float sigma[MQ], sinv[MQ];
 #pragma unroll
-    for (int i = 0; i < MQ; ++i) m[i] = NONE, ref[i] = 0.f, above[i] = -INFINITY, l[i] = zs[i] = 0.f;
+    for (int i = 0; i < MQ; ++i) {
+      m[i] = NONE, ref[i] = 0.f, above[i] = -INFINITY;
+      l[i] = zs[i] = sigma[i] = sinv[i] = 0.f;
+    }
 
     // The pages of this wave's next 32 tiles, one of their halves of 16 a lane: read one by one, each
     // tile would wait for its page before it could ask for its codes. Tokens past the end: the last
@@ -496,24 +502,15 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
           for (int i = 0; i < MQ; ++i) s[i][f] = mfma16(a, qf[i][j], s[i][f]);
         }
       __builtin_amdgcn_sched_barrier(0);  // (else all codes are spread ahead, and registers spill)
-      // does this lane's token 16 f + 4 g4 + r count at all
-      auto counts = [&](int f, int r) {
-        return !CUT || (t0 + 16 * f + 4 * g4 + r < end_t && !(off >> f & 1));
+      // does row i see this lane's token 16 f + 4 g4 + r
+      auto seen = [&](int i, int f, int r) {
+        const int t = t0 + 16 * f + 4 * g4 + r;
+        return !CUT || (t < end_t && t < see[i] && !(off >> f & 1));
       };
-      // its value scale (what stands in a place that does not count is nothing)
-      auto value_scale = [&](int f, int r) {
-        const float v = __uint_as_float(T.vp[f][r] & 0xFFFF0000u);
-        return counts(f, r) ? v : 0.f;
-      };
-      float svm = 0.f;
+      auto value_scale = [&](int f, int r) { return __uint_as_float(T.vp[f][r] & 0xFFFF0000u); };
+      float svm[MQ], top[MQ];
 #pragma unroll
-      for (int f = 0; f < 2; ++f)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) svm = fmaxf(svm, value_scale(f, r));
-      bool up = svm > 128.f * sigma;
-      float top[MQ];
-#pragma unroll
-      for (int i = 0; i < MQ; ++i) top[i] = -INFINITY;
+      for (int i = 0; i < MQ; ++i) svm[i] = 0.f, top[i] = -INFINITY;
 #pragma unroll
       for (int f = 0; f < 2; ++f)
 #pragma unroll
@@ -522,23 +519,23 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
 #pragma unroll
           for (int i = 0; i < MQ; ++i) {
             float v = fmaf(fmaf(-kz, qsum[i], s[i][f][r]), ks * qs[i], -ref[i]);
-            if (CUT && (t0 + 16 * f + 4 * g4 + r >= see[i] || !counts(f, r))) v = -INFINITY;
+            if (!seen(i, f, r)) v = -INFINITY;
             s[i][f][r] = v;
             top[i] = fmaxf(top[i], v);
+            svm[i] = fmaxf(svm[i], seen(i, f, r) ? value_scale(f, r) : 0.f);
           }
         }
+      bool up = false;
 #pragma unroll
-      for (int i = 0; i < MQ; ++i) up |= top[i] > above[i];
+      for (int i = 0; i < MQ; ++i) up |= top[i] > above[i] || svm[i] > 128.f * sigma[i];
       if (__any(up)) {  // new references
-        float sn = svm;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) sn = fmaxf(sn, __shfl_xor(sn, o));
-        sn = fmaxf(sn, sigma);
-        const float fs = sn > 0.f ? sigma / sn : 0.f;
-        sigma = sn;
-        sinv = sn > 0.f ? 1.f / sn : 0.f;
 #pragma unroll
         for (int i = 0; i < MQ; ++i) {
+          float sn = fmaxf(svm[i], __shfl_xor(svm[i], 16));
+          sn = fmaxf(fmaxf(sn, __shfl_xor(sn, 32)), sigma[i]);
+          const float fs = sn > 0.f ? sigma[i] / sn : 0.f;
+          sigma[i] = sn;
+          sinv[i] = sn > 0.f ? 1.f / sn : 0.f;
           float t = fmaxf(top[i], __shfl_xor(top[i], 16));
           t = fmaxf(t, __shfl_xor(t, 32));
           const float mn = fmaxf(m[i], ref[i] + t), fm = exp2f(m[i] - mn), fo = fm * fs;
@@ -572,15 +569,15 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
       for (int f = 0; f < 2; ++f)
 #pragma unroll
         for (int r = 0; r < 4; r += 2) {
-          const float s0 = value_scale(f, r) * sinv, s1 = value_scale(f, r + 1) * sinv;
+          const float v0 = value_scale(f, r), v1 = value_scale(f, r + 1);
           const float z0 = float(T.vp[f][r] & 0xFFu), z1 = float(T.vp[f][r + 1] & 0xFFu);
 #pragma unroll
           for (int i = 0; i < MQ; ++i) {
             const float p0 = __builtin_amdgcn_exp2f(s[i][f][r]);
             const float p1 = __builtin_amdgcn_exp2f(s[i][f][r + 1]);
             l[i] += p0 + p1;
-            float w0 = p0 * s0, w1 = p1 * s1;
-            if (CUT) {  // a hidden token's value may read as NaN
+            float w0 = p0 * (v0 * sinv[i]), w1 = p1 * (v1 * sinv[i]);
+            if (CUT) {  // a hidden token's value may read as NaN, or be far above sigma
               if (s[i][f][r] == -INFINITY) w0 = 0.f;
               if (s[i][f][r + 1] == -INFINITY) w1 = 0.f;
             }
@@ -675,7 +672,8 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
             const float z = __shfl(zs[i], 4 * g4 + r);
             sum[u] = __shfl(l[i], 4 * g4 + r), mm[u] = __shfl(m[i], 4 * g4 + r);
             // (a row that sees nothing: zeros)
-            const float f = !alone ? sigma : sum[u] == 0.f ? 0.f : sigma / sum[u];
+            const float sg = __shfl(sigma[i], 4 * g4 + r);
+            const float f = !alone ? sg : sum[u] == 0.f ? 0.f : sg / sum[u];
             float x[ND];
 #pragma unroll
             for (int d = 0; d < ND; ++d) x[d] = f * (acc[i][d][r] * (d & 1 ? 0x1p20f : 0x1p24f) - z);
@@ -736,11 +734,11 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float z = __shfl(zs[i], 4 * g4 + r);
+        const float z = __shfl(zs[i], 4 * g4 + r), sg = __shfl(sigma[i], 4 * g4 + r);
 #pragma unroll
         for (int d = 0; d < ND; ++d)
           o[(4 * g4 + r) * LD + channel(d)] =
-              sigma * (acc[i][d][r] * (d & 1 ? 0x1p20f : 0x1p24f) - z);
+              sg * (acc[i][d][r] * (d & 1 ? 0x1p20f : 0x1p24f) - z);
       }
     }
     __syncthreads();

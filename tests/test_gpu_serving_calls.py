@@ -272,3 +272,27 @@ def codes_of(words, dim):
     """The codes of packed key words."""
     w = words.reshape(-1, dim // 8, 1) >> (4 * np.arange(8, dtype=np.uint32))
     return (w & 15).reshape(-1, dim).astype(np.int64)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("heads,new,at", [(8, 100, 50), (8, 100, 99), (2, 40, 17), (1, 5, 3),
+                                          (4, 300, 131)])
+@pytest.mark.parametrize("size", [2.0 ** 40, 1e36])
+def test_values_of_later_tokens_do_not_reach_earlier_rows(dim, heads, new, at, size):
+    """One token's value far above all others: the queries before it are as exact as without it, those
+    after it see it."""
+    c = Cache([new + 7], 1, dim, 16, True, seed=41)
+    v = f64(c.v)
+    v[at + 7] *= size
+    v = torch.from_numpy(v).to(BF16)
+    slots = [int(c.table[0, t // 16]) * 16 + t % 16 for t in range(new + 7)]
+    K.kronq_cache_append(c.k.to(DEV), v.to(DEV), torch.tensor(slots, dtype=torch.int64, device=DEV),
+                         c.codes, c.params)
+    c.held[1] = O.cache_grid(f64(v), True)[3] @ (O.hadamard(dim) / np.sqrt(dim))
+    q = randn(new, heads, dim, seed=42)
+    note(f"a later token's value dim={dim} heads={heads} new={new} at={at} size={size}")
+    o = K.kronq_cache_attention(q.to(DEV), *c.dev(), torch.tensor([0, new], dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    ref = c.ref(f64(q), [0, new])
+    row = np.linalg.norm(ref, axis=-1, keepdims=True)
+    assert rel_frob(f64(o) / row, ref / row) < TOL_ATTENTION
