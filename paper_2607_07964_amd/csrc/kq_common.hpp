@@ -70,6 +70,19 @@ int launch(const char* name, Kernel kernel, dim3 grid, dim3 block, size_t shmem,
   return KRONQ_OK;
 }
 
+// The grid of n workgroups numbered by workgroup(): a dimension of a grid holds fewer than 2^32
+// work-items, so that more than 2^21 workgroups stand in rows of as many (the last row may go past n).
+inline dim3 grid_of(int64_t n) {
+  const int64_t x = int64_t(1) << 21;
+  return n <= x ? dim3(static_cast<unsigned>(n))
+                : dim3(static_cast<unsigned>(x), static_cast<unsigned>((n + x - 1) / x));
+}
+#ifdef __HIPCC__
+__device__ __forceinline__ int64_t workgroup() {
+  return blockIdx.x + int64_t(gridDim.x) * blockIdx.y;
+}
+#endif
+
 // ---- workspace carving -----------------------------------------------------------------------
 struct Carver {
   char* base;

@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256) void cache_append(AppendArgs A) {
   constexpr int LPR = DIM / 8, RPW = 256 / LPR;  // lanes per row, rows per workgroup
   const int l = threadIdx.x % LPR;
   const int chunk = chunk_of(l);
-  const int64_t row = int64_t(blockIdx.x) * RPW + threadIdx.x / LPR;  // token, head, key or value
+  const int64_t row = workgroup() * RPW + threadIdx.x / LPR;  // token, head, key or value
   const int64_t rows = A.n_tokens * A.n_kv * 2;
   if (row >= rows) return;  // (whole groups of LPR lanes)
   const int part = int(row & 1);
@@ -834,7 +834,7 @@ int cache_append_launch(const AppendJob& j, hipStream_t s) {
   a.n_kv = int(j.n_kv), a.page_log = __builtin_ctzll(uint64_t(j.page));
   a.n_slots = j.n_pages * j.page, a.slots = j.slots, a.codes = j.codes, a.params = j.params;
   a.rotate = j.rotate, a.norm = 1.0 / std::sqrt(double(j.dim)), a.k_hat = j.k_hat, a.v_hat = j.v_hat;
-  const dim3 grid(static_cast<unsigned>(cdiv(j.n_tokens * j.n_kv * 2, 2048 / j.dim)));
+  const dim3 grid = grid_of(cdiv(j.n_tokens * j.n_kv * 2, 2048 / j.dim));
   const bool half = j.dtype == KRONQ_BF16;
   if (j.dim == 128)
     return half ? launch("cache_append", cache_append<uint16_t, 128>, grid, dim3(256), 0, s, a)

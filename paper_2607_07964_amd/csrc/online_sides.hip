@@ -310,14 +310,15 @@ __global__ __launch_bounds__(in_threads(C)) void linear_in(LinearIn A, int table
   __shared__ int sh[TABLE_LDS];  // (also a workgroup's threads, or the factor)
   static_assert(TABLE_LDS >= THR && TABLE_LDS >= 784);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (int(blockIdx.x) < lead) {
-    if (int(blockIdx.x) < table_blocks) fill_table<THR>(A, blockIdx.x, sh);
-    if (int(blockIdx.x) == lead - 1 && A.offsets) list_tiles(A, sh);
+  const int64_t group = workgroup();
+  if (group < lead) {
+    if (group < table_blocks) fill_table<THR>(A, group, sh);
+    if (group == lead - 1 && A.offsets) list_tiles(A, sh);
     return;
   }
-  // The rows of a unit on one XCD (workgroup % 8; lead is a multiple of 8), one after another: a
+  // The rows of a unit on one XCD (group % 8; lead is a multiple of 8), one after another: a
   // line of the result holds 8 rows, and is then complete before it leaves that XCD's L2.
-  const int64_t b = int64_t(blockIdx.x) - lead, in = b >> 3;
+  const int64_t b = group - lead, in = b >> 3;
   const int64_t row = ((b & 7) + 8 * (in >> 5)) * 32 + (in & 31);
   if (row >= A.n_rows) return;
   int expert = 0;
@@ -642,7 +643,8 @@ __global__ __launch_bounds__(threads(C)) void linear_out(LinearOut A) {
   constexpr int THR = threads(C), WAVES = THR / 64, N = (64 * C + THR - 1) / THR;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int d = int(A.d_out), cols = A.turn.cols;
-  const int64_t row = blockIdx.x;
+  const int64_t row = workgroup();
+  if (row >= A.n_rows) return;
   int expert = 0;
   if (A.offsets) {
     expert = expert_of(A.offsets, A.n_experts, row);
@@ -781,7 +783,8 @@ template <typename T>
 __global__ __launch_bounds__(256) void linear_out_any(LinearOut A) {
   __shared__ float small[128];
   const int tid = threadIdx.x, d = int(A.d_out);
-  const int64_t row = blockIdx.x;
+  const int64_t row = workgroup();
+  if (row >= A.n_rows) return;
   int expert = 0;
   if (A.offsets) {
     expert = expert_of(A.offsets, A.n_experts, row);
@@ -828,7 +831,7 @@ int in_typed(const LinearIn& a, hipStream_t s) {
   const int cc = a.turn.rotate ? int(a.d_in / a.turn.cols) : 0;
   const int64_t table_blocks = a.table ? cdiv(a.w_rows, TABLE_ROWS) : 0;
   const int64_t lead = cdiv(table_blocks + (a.offsets ? 1 : 0), 8) * 8;
-  const dim3 grid(static_cast<unsigned>(lead + cdiv(a.n_rows, 256) * 256));
+  const dim3 grid = grid_of(lead + cdiv(a.n_rows, 256) * 256);
 #define KQ_IN(C_, N_, F_)                                                                            \
   launch("linear_in", linear_in<T, C_, N_, F_>, grid, dim3(in_threads(C_)), C_ ? size_t(a.d_in) * 4 : 0, s, a, \
          int(table_blocks), int(lead))
@@ -867,7 +870,7 @@ int out_typed(LinearOut a, hipStream_t s) {
   const size_t pair = 2 * sizeof(T);
   a.pairs = aligned(a.y, pair) && a.ldy % 2 == 0 && aligned(a.bias, 8) &&
             (!a.residual || (aligned(a.residual, pair) && a.ldr % 2 == 0));
-  const dim3 grid(static_cast<unsigned>(a.n_rows));
+  const dim3 grid = grid_of(a.n_rows);
   if (!a.turn.rotate || a.turn.cols < 8)
     return launch("linear_out", linear_out_any<T>, grid, dim3(256), 0, s, a);
 #define KQ_OUT(C_, F_) \

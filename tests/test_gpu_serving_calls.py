@@ -296,3 +296,62 @@ def test_values_of_later_tokens_do_not_reach_earlier_rows(dim, heads, new, at, s
     ref = c.ref(f64(q), [0, new])
     row = np.linalg.norm(ref, axis=-1, keepdims=True)
     assert rel_frob(f64(o) / row, ref / row) < TOL_ATTENTION
+
+
+def room_for(gigabytes):
+    if torch.cuda.mem_get_info()[0] < gigabytes * 2 ** 30 * 1.1:
+        pytest.skip("not enough free memory")
+
+
+def test_as_many_rows_as_the_limit():
+    """2^24 rows: as many workgroups of either side, of 256 threads each, are 2^32 work-items."""
+    room_for(22)
+    la = whole_numbers(5, 128, 4)
+    few = torch.randint(-8, 9, (4099, 128), generator=torch.Generator().manual_seed(1)).to(BF16).to(DEV)
+    n = 1 << 24
+    x = few.repeat(-(-n // 4099), 1)[:n].contiguous()
+    note("2^24 rows of 128")
+    y = K.kronq_online_linear(*la.args, None, None, None, None, x, flags=0)
+    torch.cuda.synchronize()
+    want = torch.from_numpy(la.ref(f64(few))).to(FP32).to(BF16).to(DEV)
+    assert torch.equal(y, want.repeat(-(-n // 4099), 1)[:n])
+    with pytest.raises(K.KronqError, match="sizes"):
+        K.kronq_online_linear(*la.args, None, None, None, None, x[:1].expand(n + 1, 128),
+                              torch.empty(1, 5, dtype=BF16, device=DEV).expand(n + 1, 5), flags=0)
+
+
+def test_rows_of_28_m_past_2_22():
+    """Rows of 28 * 32 inputs take workgroups of 1024 threads."""
+    room_for(34)
+    la = Layer(3, 896, 4, 128, K.ROT_IN)
+    few = rows_of(1021, 896, BF16)
+    n = (1 << 22) + 300
+    x = few.to(DEV).repeat(-(-n // 1021), 1)[:n].contiguous()
+    note("rows of 896 past 2^22")
+    y = K.kronq_online_linear(*la.one(), x, bias=la.bias_d[0], flags=K.ROT_IN)
+    torch.cuda.synchronize()
+    ref = la.ref(f64(few))
+    for a in (0, 1021 * 2054, 1021 * 4107):  # whole repetitions from the first to the last one
+        assert rel_frob(f64(y[a:a + 1021]), ref) < TOL[BF16]
+    assert rel_frob(f64(y[1021 * 4108:]), ref[:n - 1021 * 4108]) < TOL[BF16]
+
+
+def test_append_of_many_rows():
+    """Tokens times heads past 2^27, of which some are written: the first and the last ones."""
+    room_for(35)
+    kv, n = 2048, 65536 + 3
+    k = torch.empty(n, kv, 128, dtype=BF16, device=DEV)
+    at = [0, 1, 40000, n - 2, n - 1]
+    k[at] = randn(len(at), kv, 128, seed=51).to(DEV)
+    slots = torch.full((n,), -1, dtype=torch.int64, device=DEV)
+    slots[at] = torch.tensor([3, 15, 0, 7, 8], device=DEV)
+    codes, params = K.kronq_cache_empty(1, kv, 128, 16, DEV)
+    note("append of 2^27 rows")
+    K.kronq_cache_append(k, k, slots, codes, params)
+    few = K.kronq_cache_empty(1, kv, 128, 16, DEV)
+    K.kronq_cache_append(k[at], k[at], slots[at], *few)
+    torch.cuda.synchronize()
+    assert torch.equal(codes, few[0]) and torch.equal(params, few[1])
+    held = O.cache_grid(f64(k[n - 1, :3]), True)
+    assert np.array_equal(codes_of(codes[0, :3, 0].cpu().numpy().view(np.uint32).reshape(3, 16, 16)[:, 8],
+                                   128), held[0])
