@@ -12,6 +12,8 @@ struct LinearTile {
   int expert, unit, lo, hi;
 };
 
+constexpr int LINEAR_BLOCK = 256;  // rows of W of an item
+
 // The outputs are cut into items of a row tile and a block of rows of W, tile after tile, which
 // `workers` workgroups share: whole items in full rounds, and the groups of columns of the items left
 // over in equal parts, `per` groups a worker in item order. So the last round is as full as the others
@@ -28,15 +30,6 @@ __host__ __device__ inline LinearDeal linear_deal(int items, int ng, int workers
   if (per < 2) per = 2;
   if (per * 10 > ng * 9) per = ng;
   return LinearDeal{full, per};
-}
-
-// Column (of a chunk of 32) of element i of step jj of a lane's eight codes, in the order in which
-// the codes of a packed chunk are spread to pairs of fp16.
-__host__ __device__ inline int chunk_col(int bits, int jj, int i) {
-  const int p = i >> 1, b = i & 1;
-  if (bits == 2) return 16 * (jj >> 1) + 4 * (jj & 1) + p + 8 * b;
-  if (bits == 8) return 8 * jj + 4 * (p >> 1) + (p & 1) + 2 * b;
-  return 8 * jj + p + 4 * b;  // 3 and 4 bits
 }
 
 // A side's transform of d elements: columns of cols = min(m, 512) elements, d / cols of them.
@@ -78,10 +71,10 @@ int linear_in_launch(const LinearIn& a, hipStream_t s);
 // y = act(diag(mul_out) T_out y' + bias) + residual
 struct LinearOut {
   // y' [row][ld] (with w_unit: to be multiplied by it); dealt (workers > 0), with the parts that workers
-  // keep, [worker][32 nt][block]
+  // keep, [worker][32 nt][LINEAR_BLOCK]
   const float* part;
   int64_t ld;
-  int workers, ng, nt, block, row_blocks, items;  // items without offsets
+  int workers, ng, nt, row_blocks, items;  // items without offsets
   const float* kept;
   const float* w_unit;
   const LinearTile* tiles;

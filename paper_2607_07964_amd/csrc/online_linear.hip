@@ -47,7 +47,7 @@ __host__ __device__ inline int64_t most_tiles(int64_t n_rows, int64_t n_experts,
   return (cdiv(n_rows, 32) + e - 1) / nt + e;
 }
 
-constexpr int BLOCK = 256;  // rows of W of an item
+constexpr int BLOCK = LINEAR_BLOCK;
 
 // ---- 2. products ---------------------------------------------------------------------------------
 struct MmArgs {
@@ -57,7 +57,6 @@ struct MmArgs {
   int64_t plane;
   int ng;             // groups of 128 columns
   const uint32_t* table;  // SCALED
-  const float* w_unit;
   const float *scales, *zeros;  // otherwise
   int64_t ldsz;
   int gpq;
@@ -690,8 +689,7 @@ struct Ws {
   size_t bytes;
 };
 
-Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts,
-         bool grouped) {
+Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts) {
   Carver cv(ws);
   Ws w;
   w.xf = cv.take<uint16_t>(size_t(p.planes) * size_t(cdiv(n_rows, 32) * 32) * size_t(d_in));
@@ -701,8 +699,8 @@ Ws carve(void* ws, const Plan& p, int64_t d_out, int64_t d_in, int64_t n_rows, i
   const size_t w_rows = p.scaled ? size_t(n_experts) * size_t(d_out) : 0;
   w.w_unit = cv.take<float>(w_rows);
   w.table = cv.take<uint32_t>(w_rows * size_t(d_in / 128));
-  w.tiles = cv.take<Tile>(grouped ? size_t(p.tiles) + 1 : 0);
-  w.first = cv.take<int2>(grouped ? size_t(n_experts) : 0);
+  w.tiles = cv.take<Tile>(size_t(p.tiles) + 1);
+  w.first = cv.take<int2>(size_t(n_experts));
   w.bytes = align256(cv.used) + 256;
   return w;
 }
@@ -724,7 +722,7 @@ size_t linear_ws_bytes(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_ex
   size_t most = n_experts == 1 && n_rows <= GEMV_ROWS ? online_ws_bytes(d_out, d_in, n_rows) : 0;
   for (int t : {KRONQ_BF16, KRONQ_FP32}) {
     const Plan p = make_plan(d_out, d_in, n_rows, n_experts, t);
-    const size_t b = carve(nullptr, p, d_out, d_in, n_rows, n_experts, true).bytes;
+    const size_t b = carve(nullptr, p, d_out, d_in, n_rows, n_experts).bytes;
     most = b > most ? b : most;
   }
   return most;
@@ -746,7 +744,7 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
     return linear_out_launch(o, s);
   }
   const Plan p = make_plan(j.d_out, j.d_in, j.n_rows, j.n_experts, j.y_dtype);
-  const Ws w = carve(ws, p, j.d_out, j.d_in, j.n_rows, j.n_experts, true);
+  const Ws w = carve(ws, p, j.d_out, j.d_in, j.n_rows, j.n_experts);
   LinearIn a{};
   a.x = j.x, a.x_dtype = j.x_dtype, a.ldx = j.ldx, a.n_rows = j.n_rows, a.d_in = j.d_in;
   a.mul = j.mul_in, a.q28 = j.q28_in, a.turn = linear_turn(j.d_in, (j.flags & KRONQ_ROT_IN) != 0);
@@ -760,7 +758,7 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
   KQ_TRY(linear_in_launch(a, s));
   MmArgs m{};
   m.packed = j.packed, m.ldp = j.ldp, m.d_out = j.d_out, m.w_rows = a.w_rows;
-  m.xf = w.xf, m.plane = a.plane, m.ng = a.ng, m.table = w.table, m.w_unit = w.w_unit;
+  m.xf = w.xf, m.plane = a.plane, m.ng = a.ng, m.table = w.table;
   m.scales = j.scales, m.zeros = j.zeros, m.ldsz = j.ldsz, m.gpq = a.gpq;
   m.tiles = j.offsets ? w.tiles : nullptr, m.n_rows = j.n_rows;
   m.row_blocks = int(p.row_blocks);
@@ -769,7 +767,7 @@ int linear_launch(const LinearJob& j, void* ws, hipStream_t s) {
          : j.bits == 3 ? launch_mm<3>(m, p, s)
          : j.bits == 4 ? launch_mm<4>(m, p, s)
                        : launch_mm<8>(m, p, s));
-  o.part = w.part, o.ld = m.ld, o.block = BLOCK;
+  o.part = w.part, o.ld = m.ld;
   o.row_unit = w.row_unit;
   o.workers = p.workers, o.ng = a.ng, o.nt = p.nt, o.row_blocks = m.row_blocks, o.kept = w.kept;
   o.items = int(p.tiles * p.row_blocks), o.w_unit = p.scaled ? w.w_unit : nullptr;

@@ -430,8 +430,10 @@ __global__ __launch_bounds__(in_threads(C)) void linear_in(LinearIn A, int table
       o[k] = v[8 * n + k] * up;
       asm("" : "+v"(o[k]));  // both planes from the one rounded product (a multiplication merged
     }                        // into one conversion only would round the planes' sum twice)
-    // octet oc of its chunk of 32 columns is step oc of the codes, in the order of chunk_col; with
-    // 2 bits a step takes four columns of either of two octets, which lie in neighbouring lanes
+    // Octet oc of its chunk of 32 columns is step oc of the codes, its elements in the order in which a
+    // packed chunk's codes are spread to pairs of fp16: columns k and k + 4 (3 and 4 bits), k and k + 2
+    // of either half (8 bits); with 2 bits a step takes columns k and k + 8, four of either of two octets,
+    // which lie in neighbouring lanes.
     float t[8];
     if (A.bits == 2) {
       const bool odd = octet & 1;
@@ -531,15 +533,14 @@ struct Products {
   }
   // the workers after the first one that hold parts of element j's item: [from, to)
   __device__ __forceinline__ void parts(int j, int& from, int& to) const {
-    const int r = item0 + int(unsigned(j) / unsigned(A.block)) - full_items;
+    const int r = item0 + int(unsigned(j) / unsigned(LINEAR_BLOCK)) - full_items;
     from = to = 0;
     if (r < 0) return;
     from = r * A.ng / per + 1, to = ((r + 1) * A.ng - 1) / per + 1;
     to = to < A.workers ? to : A.workers;
   }
   __device__ __forceinline__ const float* kept(int worker, int j) const {
-    return A.kept + (int64_t(worker) * 32 * A.nt + in_tile) * A.block +
-           (j & (A.block - 1));  // (128 or 256)
+    return A.kept + (int64_t(worker) * 32 * A.nt + in_tile) * LINEAR_BLOCK + (j & (LINEAR_BLOCK - 1));
   }
   // eight neighbours
   __device__ __forceinline__ void sum8(int j, float* v) const {
