@@ -79,7 +79,7 @@ inline dim3 grid_of(int64_t n) {
 }
 #ifdef __HIPCC__
 __device__ __forceinline__ int64_t workgroup() {
-  return blockIdx.x + int64_t(gridDim.x) * blockIdx.y;
+  return blockIdx.x + (int64_t(blockIdx.y) << 21);  // (gridDim would be a load before anything else)
 }
 #endif
 
