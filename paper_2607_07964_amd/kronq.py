@@ -144,12 +144,12 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(0)
 
 
-def _row_stride(t: torch.Tensor, least: int) -> int:
-    """Row stride of a 2-D tensor; that of a single row is free (``least`` stands for it), and so is
-    the column stride of a single column."""
-    rows, cols = t.shape
-    if rows == 0 or cols == 1 or t.stride(1) == 1:
-        return t.stride(0) if rows > 1 else least
+def _row_stride(t: torch.Tensor, rows: int, cols: int) -> int:
+    """Row stride of t [rows x cols]; that of a single row is free, and so is the column stride of a
+    single column."""
+    row, col = t.stride()
+    if col == 1 or cols == 1 or rows == 0:
+        return row if rows > 1 else cols
     raise ValueError("expected a row-major 2-D tensor (unit column stride)")
 
 
@@ -507,15 +507,17 @@ def _served(func, packed, scales, zeros, bits, group, d_in, mul_in, mul_out, q28
         raise ValueError(f"x must be [rows x {d_in}]")
     n = x.shape[0]
     if y is None:
-        y = torch.empty(n, d_out, dtype=out_dtype or x.dtype, device=dev)
+        y, ldy = torch.empty(n, d_out, dtype=out_dtype or x.dtype, device=dev), d_out
     elif out_dtype not in (None, y.dtype):
         raise ValueError(f"y is {y.dtype}, out_dtype {out_dtype}")
-    if y.dim() != 2 or y.shape[0] != n or y.shape[1] != d_out:
+    elif y.dim() != 2 or y.shape[0] != n or y.shape[1] != d_out:
         raise ValueError(f"y must be [{n} x {d_out}]")
+    else:
+        ldy = _row_stride(y, n, d_out)
     if residual is not None and (residual.shape != y.shape or residual.dtype != y.dtype):
         raise ValueError("residual must have y's shape and dtype")
-    ldx, ldy = _row_stride(x, d_in), _row_stride(y, d_out)
-    ldr = 0 if residual is None else _row_stride(residual, d_out)
+    ldx = _row_stride(x, n, d_in)
+    ldr = 0 if residual is None else _row_stride(residual, n, d_out)
     with _guard(dev):
         if ws is None:
             need = lib.kronq_workspace_bytes(OP_LINEAR, d_out, d_in, n) if offsets is None else \
