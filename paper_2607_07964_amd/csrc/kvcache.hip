@@ -343,8 +343,9 @@ __global__ __launch_bounds__(256, 2) void cache_attention(AttnArgs A) {
   const int* table = A.table + int64_t(b) * A.ldt;
   const int page_mask = (1 << A.page_log) - 1;
   // later rows see more tokens: they go first, of all sequences (by sequences, the last ones of a long
-  // sequence late in the grid ran alone at the end: 244 us for prompts of 2048 to 274 tokens and 32
-  // heads, 170 this way; strictly by the tokens that rows see it was 181)
+  // sequence late in the grid ran alone at the end: 244 us in a trace for prompts of 2048 to 274 tokens
+  // and 32 heads, 170 this way; strictly by the tokens that rows see it was 181; not traced, a call of
+  // the present kernel takes 162)
   const int tiles = (nrows + TILE - 1) / TILE;
   for (int tile = tiles - 1 - int(blockIdx.z / A.splits); tile >= 0; tile -= A.tiles) {
     const int row0 = tile * TILE + (BY_ROWS ? wave * ROWS : 0);

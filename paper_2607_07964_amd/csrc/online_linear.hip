@@ -17,8 +17,9 @@
 // as the exact integers c - z, each group's sum taking its fp32 scale (few rows, where the table would
 // cost more than the sums, and fp32 outputs).
 // Precision. For bf16 outputs x' (and with the table s, and its product with the exact c - z) is rounded
-// to fp16, 2^-11 against the output's own 2^-8, and summed in fp32. For fp32 outputs x' is held in two fp16 planes (value and rest: 22 bits,
-// and never coarser than 2^-32 of the row's largest value) and the weights are exact.
+// to fp16, 2^-11 against the output's own 2^-8, and summed in fp32, parts of split columns included (as
+// fp16 they were 2% faster for 8192 rows). For fp32 outputs x' is held in two fp16 planes (value and
+// rest: 22 bits, and never coarser than 2^-32 of the row's largest value) and the weights are exact.
 #include <cmath>
 #include <type_traits>
 
@@ -415,7 +416,7 @@ __global__ __launch_bounds__(512, 2) void linear_few(MmArgs A) {
 //     of LDS and 256 registers a lane each), so that one wave's spreading of codes runs beside the
 //     other's matrix instructions.
 //   PLANES = 2, NT = 2, RT = 2: the same for fp32 results.
-// 8192 rows of 4096 x 4096 at 4 bits: 240 us, 1.15 PFLOP/s, where a large plain matrix product reaches
+// 8192 rows of 4096 x 4096 at 4 bits: 250 us, 1.10 PFLOP/s, where a large plain matrix product reaches
 // 1.22 to 1.32. A lane reads its row of W in batches; the fp32 scales and zeros (not SCALED) come
 // through LDS eight groups at a time, since 32 rows lie in 32 lines of either.
 template <int BITS, int NT, int PLANES, bool SCALED>
@@ -667,9 +668,10 @@ Plan make_plan(int64_t d_out, int64_t d_in, int64_t n_rows, int64_t n_experts, i
   p.planes = y_dtype == KRONQ_BF16 ? 1 : 2;
   // A tile of 32 rows for up to 32 rows (of an expert); more rows share the spread codes in tiles of
   // 64, or of 128 with the table, which pays for itself late: one layer at 4 bits takes, in tiles of
-  // 64 and of 128, 36 and 43 us for 256 rows of 4096 x 4096, 71 and 72 us for 256 rows of 14336 x
-  // 4096, 125 and 106 us for 512 of these; 8 experts of 14336 x 4096 take 169 and 163 us for 64 rows
-  // each, 207 and 178 us for 80 each.
+  // 64 and of 128, 36 and 49 us for 256 rows of 4096 x 4096, 73 and 76 us for 256 rows of 14336 x
+  // 4096, 126 and 111 us for 512 of these; 8 experts of 14336 x 4096 take 169 and 174 us for 64 rows
+  // each, 204 and 184 us for 80 each. (Experts of one size: how many rows each has is known on the
+  // device only, and the mean decides.)
   const int64_t rows = cdiv(n_rows, n_experts);
   p.scaled = p.planes == 1 && rows > (n_experts == 1 ? 256 : 64);
   p.nt = p.scaled ? 4 : rows > 32 ? 2 : 1;
