@@ -355,3 +355,64 @@ def test_append_of_many_rows():
     held = O.cache_grid(f64(k[n - 1, :3]), True)
     assert np.array_equal(codes_of(codes[0, :3, 0].cpu().numpy().view(np.uint32).reshape(3, 16, 16)[:, 8],
                                    128), held[0])
+
+
+def test_attention_of_more_tiles_than_a_grid_dimension():
+    """A sequence of 12.8 million rows of one kv head: more tiles than the grid's last dimension holds.
+    Only the last queries see tokens."""
+    room_for(8)
+    c = Cache([40], 1, 64, 16, True, seed=61)
+    n, heads = 200_000, 64
+    q = torch.full((n, heads, 64), 2.0, dtype=BF16, device=DEV)
+    last = randn(40, heads, 64, seed=62)
+    q[n - 40:] = last.to(DEV)
+    note("attention of 12.8 million rows")
+    o = K.kronq_cache_attention(q, *c.dev(), torch.tensor([0, n], dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    assert not bool(o[:n - 40].any())
+    assert rel_frob(f64(o[n - 40:]), c.ref(f64(last), [0, 40])) < TOL_ATTENTION
+
+
+def test_decode_of_as_many_sequences_as_the_limit():
+    """65535 sequences that share pages, of every length up to 48."""
+    c = Cache([48], 1, 64, 16, True, seed=63)
+    codes, params, table, _ = c.dev()
+    n = 65535
+    lengths = (torch.arange(n, device=DEV) % 49).to(torch.int32)
+    q = randn(1, 2, 64, seed=64).repeat(n, 1, 1)
+    note("decode of 65535 sequences")
+    o = K.kronq_cache_attention(q.to(DEV), codes, params, table.expand(n, -1).contiguous(), lengths)
+    torch.cuda.synchronize()
+    k, v = c.held
+    for length in range(49):
+        ref = O.causal_attention(f64(q[:1]), k[:length], v[:length], 64 ** -0.5)
+        mine = o[length::49]
+        assert bool((mine == mine[0]).all())
+        assert rel_frob(f64(mine[:1]), ref) < TOL_ATTENTION if length else not bool(mine.any())
+
+
+def walsh(x):
+    """H x / sqrt(d) along the last axis."""
+    d = x.shape[-1]
+    y, s = x.copy(), 1
+    while s < d:
+        a = y.reshape(*x.shape[:-1], d // (2 * s), 2, s)
+        y = np.concatenate((a[..., :1, :] + a[..., 1:, :], a[..., :1, :] - a[..., 1:, :]), -2).reshape(x.shape)
+        s *= 2
+    return y / np.sqrt(d)
+
+
+@pytest.mark.parametrize("rows", [2, 6, 300])
+@pytest.mark.parametrize("ydt", [BF16, FP32])
+@pytest.mark.parametrize("d_out,d_in,flags", [(24, 32768, K.ROT_IN), (32768, 128, K.ROT_OUT)])
+def test_the_largest_sides(rows, ydt, d_out, d_in, flags):
+    la = Layer(d_out, d_in, 4, 128, flags)
+    x = rows_of(rows, d_in, BF16)
+    note(f"{d_out}x{d_in} rows={rows} {ydt}")
+    y = K.kronq_online_linear(*la.one(), x.to(DEV), bias=la.bias_d[0], flags=flags, out_dtype=ydt)
+    torch.cuda.synchronize()
+    w = O.dequantize(la.codes[0], la.scales[0].astype(np.float64), la.zeros[0].astype(np.float64), 128)
+    t = f64(x) * la.mul_in[0]
+    t = (walsh(t) if flags & K.ROT_IN else t) @ w.T
+    ref = (walsh(t) if flags & K.ROT_OUT else t) * la.mul_out[0] + la.bias[0]
+    assert rel_frob(f64(y), ref) < TOL[ydt]
